@@ -27,6 +27,7 @@ import torch
 own = False
 
 SOFTMAX, SIGMOID = 0, 1
+_DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
 
 
 # ---------------------------------------------------------------------------------------- cases
@@ -35,8 +36,8 @@ def _linear(T, N, K, y="bf16", **kw):
     return {"op": "linear", "T": T, "N": N, "K": K, "y": y, **kw}
 
 
-def _linear_backward(T, N, K, **kw):
-    return {"op": "linear_backward", "T": T, "N": N, "K": K, **kw}
+def _linear_backward(T, N, K, dw="bf16", **kw):
+    return {"op": "linear_backward", "T": T, "N": N, "K": K, "dw": dw, **kw}
 
 
 def _swiglu(op, T, I, **kw):
@@ -57,8 +58,9 @@ def listed():
         _linear(777, 1536, 2048, y="f32", name="linear_chunk_777"),
         # the largest prompt chunk, and the forward pass of a large training batch
         _linear(8192, 4096, 7168, name="linear_prompt_8192"),
-        # a small ragged training batch: both gradients of a Qwen3-shaped projection
-        _linear_backward(1500, 1536, 2048, name="linear_backward_1500"),
+        # a small ragged training batch: both gradients of a Qwen3-shaped projection, the weight's kept
+        # in float32 as an optimizer takes it
+        _linear_backward(1500, 1536, 2048, dw="f32", name="linear_backward_1500"),
         # a large training batch: both gradients of the DeepSeek-V3-shaped down projection
         _linear_backward(8192, 7168, 2048, name="linear_backward_8192"),
         # a short ragged training batch between the two projections
@@ -92,7 +94,8 @@ def draw(rng):
             N, K = max(128, N // 128 * 128), K // 128 * 128
         most = _MAX_FLOPS // (2 * N * K * (2 if op == "linear_backward" else 1))
         T = _log(rng, 1, max(1, min(8192, most)))
-        return _linear(T, N, K, y=rng.choice(("bf16", "f32"))) if op == "linear" else _linear_backward(T, N, K)
+        kind = rng.choice(("bf16", "f32"))
+        return _linear(T, N, K, y=kind) if op == "linear" else _linear_backward(T, N, K, dw=kind)
     if op in ("swiglu", "swiglu_backward"):
         return _swiglu(op, _log(rng, 1, 8192), 128 * _log(rng, 1, 32))
     E = rng.choice((8, 60, 64, 128, 160, 256, 384, 512))
@@ -213,7 +216,7 @@ def prepare(case, seed):
         w, s = _weight(N, K, g)
         if op == "linear":
             st |= {"x": _activations(T, K, g), "w": w, "s": s,
-                   "out": torch.empty(T, N, dtype=torch.bfloat16 if case["y"] == "bf16" else torch.float32, device="cuda")}
+                   "out": torch.empty(T, N, dtype=_DTYPES[case["y"]], device="cuda")}
         else:
             # the transposed weight and the forward pass's column form of x, as a training loop keeps them
             wt = torch.zeros(K, _up128(N), dtype=torch.uint8, device="cuda")
@@ -221,7 +224,7 @@ def prepare(case, seed):
             st |= {"wt": wt, "st": s.t().contiguous(), "x_col": _quantize(_activations(T, K, g).float().t()),
                    "dy": (_activations(T, N, g).float() * 1e-3).to(torch.bfloat16),
                    "dx": torch.empty(T, K, dtype=torch.bfloat16, device="cuda"),
-                   "dw": torch.empty(N, K, dtype=torch.float32, device="cuda")}
+                   "dw_out": torch.empty(N, K, dtype=_DTYPES[case["dw"]], device="cuda")}
     elif op in ("swiglu", "swiglu_backward"):
         gu = _activations(case["T"], 2 * case["I"], g)
         if op == "swiglu":
@@ -248,7 +251,7 @@ def _plain_linear_backward(st):
     T, N, K = st["T"], st["N"], st["K"]
     dx = _values(*_quantize(dy))[:, :N] @ _weight_values(st["wt"], st["st"], K, N).t()
     dw = _values(*_quantize(dy.t()))[:, :T] @ _values(*st["x_col"])[:, :T].t()
-    return {"dx": dx.to(torch.bfloat16), "dw": dw}
+    return {"dx": dx.to(torch.bfloat16), "dw": dw.to(_DTYPES[st["dw"]])}
 
 
 def _plain_swiglu(st):
@@ -320,8 +323,8 @@ def _own(st):
         ftm.ft_act_quantize(st["dy"], T, N, st["row"], st["col"])
         ftm.ft_linear({"out_features": K, "in_features": N, "x_dtype": ftm.FT_DT_FP8_ACT, "y_dtype": ftm.FT_DT_BF16},
                       {"w": st["wt"], "s": st["st"]}, st["row"], T, st["dx"])
-        ftm.ft_linear_weight_grad(N, K, T, st["col"], _own_form(st["x_col"], K, T), st["dw"])
-        return {"dx": st["dx"], "dw": st["dw"]}
+        ftm.ft_linear_weight_grad(N, K, T, st["col"], _own_form(st["x_col"], K, T), st["dw_out"])
+        return {"dx": st["dx"], "dw": st["dw_out"]}
     if op == "swiglu":
         if "h" not in st:
             st["h"], st["saved"] = ftm.ActCodes(T, st["I"]), ftm.ActCodes(T, 2 * st["I"])
@@ -369,7 +372,7 @@ def work(case):
         wb = N * K + 4 * (_up128(N) // 128) * (_up128(K) // 128)
         if op == "linear":
             return {"bytes": 2 * T * K + wb + T * N * (2 if case["y"] == "bf16" else 4), "flops": 2 * T * N * K}
-        return {"bytes": 2 * T * N + wb + 2 * T * K + T * K + T * K // 128 + 4 * N * K, "flops": 4 * T * N * K}
+        return {"bytes": 2 * T * N + wb + 2 * T * K + T * K + T * K // 128 + N * K * (2 if case["dw"] == "bf16" else 4), "flops": 4 * T * N * K}
     if op == "swiglu":
         return {"bytes": T * case["I"] * 7 + 3 * T * case["I"] // 128, "flops": 6 * T * case["I"]}
     if op == "swiglu_backward":
