@@ -75,9 +75,10 @@ enum {
     FT_DT_F32 = 0,              /* IEEE float32 */
     FT_DT_BF16 = 1,             /* bfloat16 */
     FT_DT_FP8E4M3FN_B128 = 2,   /* OCP fp8 e4m3fn codes, one float32 scale per 128x128 block */
-    FT_DT_MXFP4 = 3             /* OCP MXFP4: fp4 e2m1 codes, two per byte (element 2j in the low
+    FT_DT_MXFP4 = 3,            /* OCP MXFP4: fp4 e2m1 codes, two per byte (element 2j in the low
                                    nibble of byte j), one e8m0 scale byte (2^(s-127)) per 32
                                    consecutive elements of a row */
+    FT_DT_FP8_ACT = 4           /* activations in 8-bit form (ft_act_codes_t); ft_linear's x only */
 };
 
 #define FT_SLOT_MISS (-1)
@@ -468,6 +469,163 @@ ft_status_t ft_prefill_layers(const ft_moe_desc_t *desc, int32_t n_layers,
                               const void *const *x, int32_t T, float *const *out,
                               const ft_route_t *route, void *ws, size_t ws_bytes, int32_t overlap,
                               void *stream, void *copy_stream);
+
+/*
+ * ---- Dense layers next to the experts, in the experts' 8-bit arithmetic: products, what their backward
+ * pass keeps and reads, and the router's balance loss.
+ *
+ * 8-bit form of a matrix of R rows and K columns (device pointers, caller-owned, 16-byte aligned).
+ * With Kp and Rp for K and R rounded up to multiples of 128 (FT_ACT_PAD):
+ *   codes  [R][Kp]       e4m3fn codes; those of columns K .. Kp - 1 are 0
+ *   scales [Kp/128][Rp]  e8m0 bytes: code (r, c) stands for e4m3fn(code) * 2^(scales[c/128][r] - 127);
+ *                        entries of rows R .. Rp - 1 are written (127) but stand for nothing
+ * The rule is FT_ACT_FP8_1x128_POW2's: per row and block of 128 columns the smallest power of two
+ * 2^e with 448 * 2^e >= the block's largest finite magnitude (e = 0 for a block of zeros, clamped to
+ * [-127, 127]), values rounded to nearest, ties to even, in one step from the source's precision;
+ * an infinity or NaN becomes a NaN code.  The scales of one block of consecutive rows are
+ * contiguous, so a product moves those of a tile with one load.  The row form of a matrix [T][C]
+ * is this form of it (R = T, K = C), the column form that of its transpose (R = C, K = T), whose
+ * blocks of 128 run along the tokens.
+ *
+ * Sizes of all calls below: feature counts are multiples of 16 from 16 to 65536 (inter: a multiple of 128
+ * up to 32768), 0 <= T <= 1048576, FT_ERR_SHAPE otherwise; where nothing else is said T == 0 enqueues
+ * nothing.  Matrices are contiguous and row-major, all array pointers 16-byte aligned except those
+ * of float32 weight scales and of the router's arrays (FT_ERR_SHAPE otherwise).  Outputs must not
+ * overlap inputs.
+ */
+#define FT_ACT_PAD(n) (((n) + 127) / 128 * 128)
+typedef struct {
+    uint8_t *codes;
+    uint8_t *scales;
+} ft_act_codes_t;
+
+/*
+ * The row form of x [T][C] (x_dtype FT_DT_BF16 or FT_DT_F32), its column form, or both from one read of
+ * x; the form whose argument is NULL is left out.  The row form is what ft_linear takes with
+ * FT_DT_FP8_ACT; the column forms of a product's input, kept from the forward pass at 8 bits an
+ * element, and of its output's gradient are what ft_linear_weight_grad reads.
+ */
+ft_status_t ft_act_quantize(const void *x, int32_t x_dtype, int32_t T, int32_t C, const ft_act_codes_t *row,
+                            const ft_act_codes_t *col, void *stream);
+
+/*
+ * Dense product y[T][N] = x[T][K] W[N][K]^T, N = out_features, K = in_features, over a weight in the
+ * experts' format and activations in 8 bits (a shared expert's or a dense layer's projections).
+ *   w         [N][Kp] e4m3fn codes (Kp as above; codes of the padding columns 0; for K a multiple
+ *             of 128 a bank row of ft_banks_t), w_scales [ceil(N/128)][Kp/128] float32:
+ *             weight (r, c) = code(r, c) * scale(r/128, c/128)
+ *   x         [T][K] in x_dtype FT_DT_BF16 or FT_DT_F32, brought into the row form by the call; or,
+ *             with FT_DT_FP8_ACT, the codes of its row form, x_scales that form's scales (NULL
+ *             and unused otherwise)
+ *   y         [T][N] in y_dtype, overwritten.  FT_DT_BF16: fp8 matrix instructions, whose sums carry
+ *             an error of about 2^-16 of the result, then one rounding to bf16.  FT_DT_F32:
+ *             products and sums exact to float32's rounding, at half the matrix rate.
+ *   ws        at least ft_linear_workspace_bytes(desc, T) bytes (FT_ERR_CAPACITY); none with
+ *             FT_DT_FP8_ACT, where that is 0 and ws may be NULL
+ * Sums run in a fixed order: results do not change between calls.  The gradient of x is the same
+ * product over the transposed weight: dx = ft_linear(out K, in N, w^T, dy).
+ * ft_linear_workspace_bytes: bytes for up to max_tokens tokens; 0 too if desc is invalid.
+ */
+typedef struct {
+    int32_t out_features, in_features, x_dtype, y_dtype;
+} ft_linear_desc_t;
+
+size_t ft_linear_workspace_bytes(const ft_linear_desc_t *desc, int32_t max_tokens);
+ft_status_t ft_linear(const ft_linear_desc_t *desc, const uint8_t *w, const float *w_scales, const void *x,
+                      const uint8_t *x_scales, int32_t T, void *y, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * The transpose of a weight of ft_linear, in the same format: wt [K][Np] (Np: N up to a multiple of 128,
+ * codes of the padding columns 0), wt_scales [ceil(K/128)][Np/128].  Exact; once per change of the weight.
+ */
+ft_status_t ft_linear_transpose(int32_t out_features, int32_t in_features, const uint8_t *w, const float *w_scales,
+                                uint8_t *wt, float *wt_scales, void *stream);
+
+/*
+ * Gradient of the weight, dw[N][K] = dy[T][N]^T x[T][K], from the column forms of dy and x.
+ *   dw_dtype   FT_DT_F32 or FT_DT_BF16, with the arithmetic of ft_linear's y_dtype
+ *   accumulate 1: added to dw (float32 only, FT_ERR_DTYPE otherwise), 0: dw overwritten
+ * T == 0 writes zeros (accumulate: leaves dw as it is).
+ */
+ft_status_t ft_linear_weight_grad(int32_t out_features, int32_t in_features, int32_t T, const ft_act_codes_t *dy_col,
+                                  const ft_act_codes_t *x_col, void *dw, int32_t dw_dtype, int32_t accumulate,
+                                  void *stream);
+
+/*
+ * SwiGLU between two dense products, with 8 bits kept for the backward pass.
+ *   gu     [T][2I] in gu_dtype (FT_DT_BF16 or FT_DT_F32), I = inter: the gate projection's I columns,
+ *          then the up projection's (the row order of ft_banks_t.w13)
+ *   h      row form [T][I] of silu(gate) * up, computed in float32 and rounded once: the next
+ *          product's input
+ *   saved  row form [T][2I] of gu, all the backward pass needs of it; NULL where there is none
+ */
+ft_status_t ft_swiglu_quantize(const void *gu, int32_t gu_dtype, int32_t T, int32_t inter, const ft_act_codes_t *h,
+                               const ft_act_codes_t *saved, void *stream);
+
+/*
+ * Its backward pass from what was kept and from dh [T][I] (dh_dtype FT_DT_BF16 or FT_DT_F32), with
+ * s = 1 / (1 + exp(-gate)):  d_gate = dh up s (1 + gate (1 - s)),  d_up = dh gate s,  h = gate s up
+ * (from the kept gate and up).  Written in 8 bits for the products that follow; NULL leaves one out:
+ *   dgu_row  row form [T][2I] of (d_gate, d_up): the input of the gradient of x
+ *   dgu_col  its column form (R = 2I, K = T): for the gate/up weight's gradient
+ *   h_col    the column form of h (R = I, K = T): for the down weight's gradient
+ */
+ft_status_t ft_swiglu_backward(const ft_act_codes_t *saved, const void *dh, int32_t dh_dtype, int32_t T, int32_t inter,
+                               const ft_act_codes_t *dgu_row, const ft_act_codes_t *dgu_col, const ft_act_codes_t *h_col,
+                               void *stream);
+
+/*
+ * Balance loss of the router over packed sequences, with per-expert counts.  For sequence s of n counted
+ * tokens, p_t the router probabilities of token t over all E experts (gating softmax: softmax of
+ * its logits; sigmoid: their sigmoids divided by their sum) and c_e the routed pairs of its tokens on e:
+ *   prob_e = (1/n) sum_t p_te,  frac_e = coef E c_e / (k n),  loss = sum_e frac_e prob_e
+ * and zeros for a sequence without counted tokens.
+ *   logits    [T][E] float32 as for ft_route_only; -inf is an expert with probability 0, and a token all of
+ *             whose logits are -inf adds no probabilities
+ *   topk_ids  [T][k] int32, the routing of these logits (ft_route_t.topk_ids); an id outside [0, E) is not
+ *             counted
+ *   seq_off   [n_seq + 1] int32 device: sequence s is tokens [seq_off[s], seq_off[s+1]); must not decrease,
+ *             tokens before the first and behind the last belong to none.  NULL: one sequence of T
+ *             tokens (n_seq 1, FT_ERR_NULL otherwise)
+ *   mask      [T] uint8 or NULL: a token with 0 is not counted (padding)
+ *   out       counts [n_seq][E] int32, tokens [n_seq] int32 (n), prob and frac [n_seq][E] float32,
+ *             loss [n_seq] float32; all overwritten, T == 0 included
+ *   ws        at least ft_balance_workspace_bytes(desc, T) bytes
+ * Limits: E and k as in ft_moe_desc_t, 1 <= n_seq <= 65536.  Sums run in a fixed order.
+ */
+typedef struct {
+    int32_t n_experts, top_k, gating, n_seq;
+    float coef;
+} ft_balance_desc_t;
+
+typedef struct {
+    int32_t *counts;
+    int32_t *tokens;
+    float *prob;
+    float *frac;
+    float *loss;
+} ft_balance_t;
+
+size_t ft_balance_workspace_bytes(const ft_balance_desc_t *desc, int32_t max_tokens);
+ft_status_t ft_balance_loss(const ft_balance_desc_t *desc, const float *logits, const int32_t *topk_ids, int32_t T,
+                            const int32_t *seq_off, const uint8_t *mask, const ft_balance_t *out, void *ws,
+                            size_t ws_bytes, void *stream);
+
+/*
+ * Gradient of the router logits: of sum_s d_loss[s] loss_s with frac held fixed (counts have no gradient),
+ * plus of the gates g = topk_w (ft_route_t.topk_w) given d_topk_w.  With a = 1 (softmax) or
+ * 1 - sigmoid(logit):
+ *   d_logits_te = d_loss_s/n p_te a_te (frac_e - sum_i frac_i p_ti) + [e = e_tj] g_j a_te (dg_j - sum_i g_i dg_i)
+ *   balance   tokens and frac are read: ft_balance_loss's, or frac from counts summed over a larger batch
+ *   d_loss    [n_seq] float32, or NULL: without the loss (balance may be NULL)
+ *   topk_w, d_topk_w  [T][k] float32, or d_topk_w NULL: without the gates (topk_w, topk_ids may be NULL)
+ *   d_logits  [T][E] float32: rows of the sequences' tokens are overwritten (masked tokens have only
+ *             the gates' part), rows of tokens in no sequence are left as they were
+ */
+ft_status_t ft_router_backward(const ft_balance_desc_t *desc, const float *logits, const int32_t *topk_ids, int32_t T,
+                               const int32_t *seq_off, const uint8_t *mask, const ft_balance_t *balance,
+                               const float *d_loss, const float *topk_w, const float *d_topk_w, float *d_logits,
+                               void *stream);
 
 /* Static string for a status code. */
 const char *ft_status_string(ft_status_t status);

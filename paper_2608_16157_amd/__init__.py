@@ -19,11 +19,23 @@ of the C ABI declared in ``include/ftmoe.h``:
                        max_fill, step, x, T, out, route, plan, host, ws, pool, stream=None)
     ft_prefill_layers(desc, host_layers, dev_bufs, slot_table, logits, x, T, out, route, ws,
                       overlap=True, stream=None, copy_stream=None)
+    ft_act_quantize(x, T, C, row=None, col=None, stream=None)
+    ft_linear_workspace_bytes(desc, max_tokens) -> int
+    ft_linear(desc, weight, x, T, y, ws=None, stream=None)
+    ft_linear_transpose(out_features, in_features, weight, weight_t, stream=None)
+    ft_linear_weight_grad(out_features, in_features, T, dy_col, x_col, dw, accumulate=False, stream=None)
+    ft_swiglu_quantize(gu, T, inter, h, saved=None, stream=None)
+    ft_swiglu_backward(saved, dh, T, inter, dgu_row=None, dgu_col=None, h_col=None, stream=None)
+    ft_balance_workspace_bytes(desc, max_tokens) -> int
+    ft_balance_loss(desc, logits, topk_ids, T, out, ws, seq_off=None, mask=None, stream=None)
+    ft_router_backward(desc, logits, topk_ids, T, balance, d_loss, d_logits, topk_w=None, d_topk_w=None,
+                       seq_off=None, mask=None, stream=None)
     ft_status_string(status) -> str
 
 ``desc`` is a dict with the ft_moe_desc_t fields; ``route`` a RouteBuffers; ``banks`` a dict
-with w13, w2 (and s13, s2 for fp8) device tensors; everything else device tensors.  A non-OK
-status raises FtError.  If the library is not built, importing works but every call raises.
+with w13, w2 (and s13, s2 for fp8) device tensors; a ``weight`` of the dense product a dict with w and
+s; 8-bit forms ActCodes; ``ft_balance_loss``'s outputs a BalanceBuffers; everything else device
+tensors.  A non-OK status raises FtError.  If the library is not built, importing works but every call raises.
 """
 from __future__ import annotations
 
@@ -40,14 +52,16 @@ FT_OK, FT_ERR_NULL, FT_ERR_SHAPE, FT_ERR_DTYPE, FT_ERR_CAPACITY, FT_ERR_HIP = ra
 FT_GATE_SOFTMAX_TOPK_RENORM, FT_GATE_SIGMOID_TOPK_RENORM = 0, 1
 FT_COMBINE_ORDERED, FT_COMBINE_ATOMIC = 0, 1
 FT_ACT_EXACT, FT_ACT_FP8_1x128_POW2 = 0, 1
-FT_DT_F32, FT_DT_BF16, FT_DT_FP8E4M3FN_B128, FT_DT_MXFP4 = 0, 1, 2, 3
+FT_DT_F32, FT_DT_BF16, FT_DT_FP8E4M3FN_B128, FT_DT_MXFP4, FT_DT_FP8_ACT = 0, 1, 2, 3, 4
 FT_SLOT_MISS = -1
 FT_DEV_SLOT_RANGE, FT_DEV_SLOT_DUP, FT_DEV_SLOT_SHARED = 1, 2, 4
 
 EXPORTED = ("ft_moe_workspace_bytes", "ft_route_only", "ft_moe_forward", "ft_moe_forward_noalloc",
             "ft_moe_forward_profiled", "ft_miss_list_to_host", "ft_cache_plan", "ft_cpu_experts",
             "ft_cache_fill", "ft_moe_step_hybrid", "ft_prefill_layers", "ft_status_string",
-            "ft_cpu_pool_create", "ft_cpu_pool_destroy")
+            "ft_cpu_pool_create", "ft_cpu_pool_destroy", "ft_act_quantize", "ft_linear_workspace_bytes",
+            "ft_linear", "ft_linear_transpose", "ft_linear_weight_grad", "ft_swiglu_quantize",
+            "ft_swiglu_backward", "ft_balance_workspace_bytes", "ft_balance_loss", "ft_router_backward")
 FT_PROF_STAGES = 4
 FT_NOALLOC_SCRATCH_BYTES = 64 << 20
 
@@ -104,6 +118,23 @@ class ft_hybrid_host_t(ctypes.Structure):
 
 
 FT_HYBRID_TASK_BYTES = 24 * 8
+
+
+class ft_act_codes_t(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+class ft_linear_desc_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("out_features", "in_features", "x_dtype", "y_dtype")]
+
+
+class ft_balance_desc_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_experts", "top_k", "gating", "n_seq")] + \
+               [("coef", ctypes.c_float)]
+
+
+class ft_balance_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("counts", "tokens", "prob", "frac", "loss")]
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -164,6 +195,28 @@ def load(path: str = None) -> ctypes.CDLL:
                                       ctypes.c_void_p, P(ctypes.c_void_p), P(ctypes.c_void_p),
                                       ctypes.c_int32, P(ctypes.c_void_p), P(ft_route_t), ctypes.c_void_p,
                                       ctypes.c_size_t, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p]
+    p, i, z = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
+    codes, bal = P(ft_act_codes_t), P(ft_balance_t)
+    lib.ft_act_quantize.restype = ctypes.c_int
+    lib.ft_act_quantize.argtypes = [p, i, i, i, codes, codes, p]
+    lib.ft_linear_workspace_bytes.restype = z
+    lib.ft_linear_workspace_bytes.argtypes = [P(ft_linear_desc_t), i]
+    lib.ft_linear.restype = ctypes.c_int
+    lib.ft_linear.argtypes = [P(ft_linear_desc_t), p, p, p, p, i, p, p, z, p]
+    lib.ft_linear_transpose.restype = ctypes.c_int
+    lib.ft_linear_transpose.argtypes = [i, i, p, p, p, p, p]
+    lib.ft_linear_weight_grad.restype = ctypes.c_int
+    lib.ft_linear_weight_grad.argtypes = [i, i, i, codes, codes, p, i, i, p]
+    lib.ft_swiglu_quantize.restype = ctypes.c_int
+    lib.ft_swiglu_quantize.argtypes = [p, i, i, i, codes, codes, p]
+    lib.ft_swiglu_backward.restype = ctypes.c_int
+    lib.ft_swiglu_backward.argtypes = [codes, p, i, i, i, codes, codes, codes, p]
+    lib.ft_balance_workspace_bytes.restype = z
+    lib.ft_balance_workspace_bytes.argtypes = [P(ft_balance_desc_t), i]
+    lib.ft_balance_loss.restype = ctypes.c_int
+    lib.ft_balance_loss.argtypes = [P(ft_balance_desc_t), p, p, i, p, p, bal, p, z, p]
+    lib.ft_router_backward.restype = ctypes.c_int
+    lib.ft_router_backward.argtypes = [P(ft_balance_desc_t), p, p, i, p, p, bal, p, p, p, p, p]
     lib.ft_status_string.restype = ctypes.c_char_p
     lib.ft_status_string.argtypes = [ctypes.c_int]
     _lib = lib
@@ -626,3 +679,310 @@ def ft_prefill_layers(desc: dict, host_layers: list, dev_bufs: list, slot_table:
                                   arr(logits), arr(x), int(T), arr(out), ctypes.byref(route.c()),
                                   _ptr(ws), ws.numel(), 1 if overlap else 0, _stream(stream), cs)
     _check(st, "ft_prefill_layers")
+
+
+# ------------------------------------------------------------ dense layers next to the experts
+
+_FLOATS = {torch.float32: FT_DT_F32, torch.bfloat16: FT_DT_BF16}
+_CODES = (torch.uint8, torch.float8_e4m3fn)
+
+
+def _pad128(n: int) -> int:
+    return (n + 127) // 128 * 128
+
+
+class ActCodes:
+    """8-bit form of a matrix of ``rows`` x ``cols`` (ft_act_codes_t): ``codes`` uint8 [rows][Kp] and
+    ``scales`` uint8 [Kp/128][Rp], Kp and Rp being cols and rows rounded up to multiples of 128.  The row
+    form of x [T][C] is ActCodes(T, C), its column form ActCodes(C, T)."""
+
+    def __init__(self, rows: int, cols: int, device="cuda"):
+        kp = _pad128(cols)
+        self.rows, self.cols = rows, cols
+        self.codes = torch.empty(rows, kp, dtype=torch.uint8, device=device)
+        self.scales = torch.empty(kp // 128, _pad128(rows), dtype=torch.uint8, device=device)
+
+    @classmethod
+    def of(cls, codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int) -> "ActCodes":
+        """A form over existing tensors."""
+        self = cls.__new__(cls)
+        self.rows, self.cols, self.codes, self.scales = rows, cols, codes, scales
+        return self
+
+    def c(self) -> ft_act_codes_t:
+        return ft_act_codes_t(_ptr(self.codes), _ptr(self.scales))
+
+
+def _device_of(*tensors) -> torch.device:
+    """The one device of the call's tensors."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        for u in ((t.codes, t.scales) if isinstance(t, ActCodes) else (t,)):
+            if dev is None:
+                dev = u.device
+            elif u.device != dev:
+                raise ValueError(f"tensors on {dev} and {u.device}; a call works on one device")
+    return dev
+
+
+def _on(device: torch.device, call, *args) -> int:
+    """``call(*args, stream)`` with ``device`` current; the last of ``args`` is the caller's stream or
+    None for that device's current one."""
+    if device.index == torch.cuda.current_device():
+        return call(*args[:-1], _stream(args[-1]))
+    with torch.cuda.device(device):
+        return call(*args[:-1], _stream(args[-1]))
+
+
+def _need_codes(c, name: str, rows: int, cols: int) -> None:
+    if not isinstance(c, ActCodes):
+        raise ValueError(f"{name}: expected an ActCodes, got {type(c).__name__}")
+    if c.rows != rows or c.cols != cols:
+        raise ValueError(f"{name}: the form of a {c.rows} x {c.cols} matrix, the call needs {rows} x {cols}")
+    kp = _pad128(cols)
+    _need(c.codes, f"{name}.codes", _CODES, rows * kp)
+    _need(c.scales, f"{name}.scales", torch.uint8, kp // 128 * _pad128(rows))
+
+
+def _ref(c):
+    return None if c is None else ctypes.byref(c.c())
+
+
+def _need_sizes(T: int, *features: int) -> None:
+    """Sizes the library refuses (FT_ERR_SHAPE) would make the element counts here meaningless."""
+    if not 0 <= T <= 1048576 or any(not 16 <= f <= 65536 or f % 16 for f in features):
+        raise FtError(FT_ERR_SHAPE, "sizes")
+
+
+def ft_act_quantize(x: torch.Tensor, T: int, C: int, row: Optional[ActCodes] = None,
+                    col: Optional[ActCodes] = None, stream=None) -> None:
+    T, C = int(T), int(C)
+    _need_sizes(T, C)
+    if T == 0:
+        return
+    _need(x, "x", tuple(_FLOATS), T * C)
+    if row is not None:
+        _need_codes(row, "row", T, C)
+    if col is not None:
+        _need_codes(col, "col", C, T)
+    st = _on(_device_of(x, row, col), load().ft_act_quantize, _ptr(x), _FLOATS[x.dtype], T, C, _ref(row), _ref(col),
+             stream)
+    _check(st, "ft_act_quantize")
+
+
+def _linear_desc(d: dict) -> ft_linear_desc_t:
+    return ft_linear_desc_t(int(d["out_features"]), int(d["in_features"]), int(d["x_dtype"]), int(d["y_dtype"]))
+
+
+def ft_linear_workspace_bytes(desc: dict, max_tokens: int) -> int:
+    return int(load().ft_linear_workspace_bytes(ctypes.byref(_linear_desc(desc)), int(max_tokens)))
+
+
+def alloc_linear_workspace(desc: dict, max_tokens: int, device="cuda") -> Optional[torch.Tensor]:
+    """Workspace of ft_linear for up to max_tokens tokens; None where the call needs none."""
+    n = ft_linear_workspace_bytes(desc, max_tokens)
+    if n == 0 and int(desc["x_dtype"]) != FT_DT_FP8_ACT:
+        raise FtError(FT_ERR_SHAPE, "ft_linear_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def _need_weight(weight: dict, name: str, N: int, K: int) -> None:
+    kp = _pad128(K)
+    _need(weight.get("w"), f"{name}['w']", _CODES, N * kp)
+    _need(weight.get("s"), f"{name}['s']", torch.float32, _pad128(N) // 128 * (kp // 128))
+
+
+def ft_linear(desc: dict, weight: dict, x, T: int, y: torch.Tensor, ws: Optional[torch.Tensor] = None,
+              stream=None) -> None:
+    """``x``: a device tensor [T][in_features] of x_dtype, or with FT_DT_FP8_ACT its row form
+    (ActCodes)."""
+    d, T = _linear_desc(desc), int(T)
+    N, K = d.out_features, d.in_features
+    _need_sizes(T, N, K)
+    if T == 0:
+        return
+    _need_weight(weight, "weight", N, K)
+    if d.x_dtype == FT_DT_FP8_ACT:
+        _need_codes(x, "x", T, K)
+        xp, xs = x.codes, x.scales
+    else:
+        if d.x_dtype not in _X_DTYPES:
+            raise FtError(FT_ERR_DTYPE, "ft_linear")
+        _need(x, "x", _X_DTYPES[d.x_dtype], T * K)
+        _need(ws, "ws", torch.uint8, 0)
+        xp, xs = x, None
+    if d.y_dtype not in _X_DTYPES:
+        raise FtError(FT_ERR_DTYPE, "ft_linear")
+    _need(y, "y", _X_DTYPES[d.y_dtype], T * N)
+    w, s = weight["w"], weight["s"]
+    st = _on(_device_of(w, s, xp, xs, y, ws), load().ft_linear, ctypes.byref(d), _ptr(w), _ptr(s), _ptr(xp), _ptr(xs), T,
+             _ptr(y), _ptr(ws), 0 if ws is None else ws.numel(), stream)
+    _check(st, "ft_linear")
+
+
+def ft_linear_transpose(out_features: int, in_features: int, weight: dict, weight_t: dict, stream=None) -> None:
+    N, K = int(out_features), int(in_features)
+    _need_sizes(0, N, K)
+    _need_weight(weight, "weight", N, K)
+    _need_weight(weight_t, "weight_t", K, N)
+    t = (weight["w"], weight["s"], weight_t["w"], weight_t["s"])
+    st = _on(_device_of(*t), load().ft_linear_transpose, N, K, *map(_ptr, t), stream)
+    _check(st, "ft_linear_transpose")
+
+
+def ft_linear_weight_grad(out_features: int, in_features: int, T: int, dy_col: ActCodes, x_col: ActCodes,
+                          dw: torch.Tensor, accumulate: bool = False, stream=None) -> None:
+    """``dw``: float32 or bfloat16 [out_features][in_features]."""
+    N, K, T = int(out_features), int(in_features), int(T)
+    _need_sizes(T, N, K)
+    _need(dw, "dw", tuple(_FLOATS), N * K)
+    if T > 0:
+        _need_codes(dy_col, "dy_col", N, T)
+        _need_codes(x_col, "x_col", K, T)
+    else:
+        dy_col = x_col = None
+    st = _on(_device_of(dw, dy_col, x_col), load().ft_linear_weight_grad, N, K, T, _ref(dy_col), _ref(x_col), _ptr(dw),
+             _FLOATS[dw.dtype], 1 if accumulate else 0, stream)
+    _check(st, "ft_linear_weight_grad")
+
+
+def _need_inter(T: int, inter: int) -> None:
+    if inter % 128:
+        raise FtError(FT_ERR_SHAPE, "sizes")
+    _need_sizes(T, inter, 2 * inter)
+
+
+def ft_swiglu_quantize(gu: torch.Tensor, T: int, inter: int, h: ActCodes, saved: Optional[ActCodes] = None,
+                       stream=None) -> None:
+    T, I = int(T), int(inter)
+    _need_inter(T, I)
+    if T == 0:
+        return
+    _need(gu, "gu", tuple(_FLOATS), T * 2 * I)
+    _need_codes(h, "h", T, I)
+    if saved is not None:
+        _need_codes(saved, "saved", T, 2 * I)
+    st = _on(_device_of(gu, h, saved), load().ft_swiglu_quantize, _ptr(gu), _FLOATS[gu.dtype], T, I, _ref(h), _ref(saved),
+             stream)
+    _check(st, "ft_swiglu_quantize")
+
+
+def ft_swiglu_backward(saved: ActCodes, dh: torch.Tensor, T: int, inter: int, dgu_row: Optional[ActCodes] = None,
+                       dgu_col: Optional[ActCodes] = None, h_col: Optional[ActCodes] = None, stream=None) -> None:
+    T, I = int(T), int(inter)
+    _need_inter(T, I)
+    if T == 0:
+        return
+    _need_codes(saved, "saved", T, 2 * I)
+    _need(dh, "dh", tuple(_FLOATS), T * I)
+    for c, name, rows, cols in ((dgu_row, "dgu_row", T, 2 * I), (dgu_col, "dgu_col", 2 * I, T), (h_col, "h_col", I, T)):
+        if c is not None:
+            _need_codes(c, name, rows, cols)
+    st = _on(_device_of(saved, dh, dgu_row, dgu_col, h_col), load().ft_swiglu_backward, _ref(saved), _ptr(dh),
+             _FLOATS[dh.dtype], T, I, _ref(dgu_row), _ref(dgu_col), _ref(h_col), stream)
+    _check(st, "ft_swiglu_backward")
+
+
+class BalanceBuffers:
+    """Device tensors behind one ft_balance_t: counts, prob, frac [n_seq][E], tokens, loss [n_seq]."""
+
+    def __init__(self, n_seq: int, n_experts: int, device="cuda"):
+        i32, f32 = dict(dtype=torch.int32, device=device), dict(dtype=torch.float32, device=device)
+        self.counts = torch.empty(n_seq, n_experts, **i32)
+        self.tokens = torch.empty(n_seq, **i32)
+        self.prob = torch.empty(n_seq, n_experts, **f32)
+        self.frac = torch.empty(n_seq, n_experts, **f32)
+        self.loss = torch.empty(n_seq, **f32)
+
+    @classmethod
+    def of(cls, counts, tokens, prob, frac, loss) -> "BalanceBuffers":
+        """Buffers over existing tensors."""
+        self = cls.__new__(cls)
+        self.counts, self.tokens, self.prob, self.frac, self.loss = counts, tokens, prob, frac, loss
+        return self
+
+    def c(self) -> ft_balance_t:
+        return ft_balance_t(*[_ptr(getattr(self, n)) for n, _ in ft_balance_t._fields_])
+
+
+def _balance_desc(d: dict) -> ft_balance_desc_t:
+    return ft_balance_desc_t(int(d["n_experts"]), int(d["top_k"]), int(d["gating"]), int(d["n_seq"]),
+                             float(d.get("coef", 1.0)))
+
+
+def ft_balance_workspace_bytes(desc: dict, max_tokens: int) -> int:
+    return int(load().ft_balance_workspace_bytes(ctypes.byref(_balance_desc(desc)), int(max_tokens)))
+
+
+def alloc_balance_workspace(desc: dict, max_tokens: int, device="cuda") -> torch.Tensor:
+    n = ft_balance_workspace_bytes(desc, max_tokens)
+    if n == 0:
+        raise FtError(FT_ERR_SHAPE, "ft_balance_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _need_tokens(d: ft_balance_desc_t, logits, topk_ids, T: int, seq_off, mask) -> None:
+    if T < 0:
+        raise FtError(FT_ERR_SHAPE, "sizes")
+    if T > 0:
+        _need(logits, "logits", torch.float32, T * d.n_experts)
+        if topk_ids is not None:
+            _need(topk_ids, "topk_ids", torch.int32, T * d.top_k)
+        if mask is not None:
+            _need(mask, "mask", (torch.uint8, torch.bool), T)
+    if seq_off is not None:
+        _need(seq_off, "seq_off", torch.int32, d.n_seq + 1)
+
+
+def _need_balance(d: ft_balance_desc_t, b, names) -> None:
+    if not isinstance(b, BalanceBuffers):
+        raise ValueError("expected a BalanceBuffers")
+    for n in names:
+        _need(getattr(b, n), n, torch.int32 if n in ("counts", "tokens") else torch.float32,
+              d.n_seq * (1 if n in ("tokens", "loss") else d.n_experts))
+
+
+def ft_balance_loss(desc: dict, logits: torch.Tensor, topk_ids: torch.Tensor, T: int, out: BalanceBuffers,
+                    ws: torch.Tensor, seq_off: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+                    stream=None) -> None:
+    """``topk_ids``: the routing's (RouteBuffers.topk_ids); ``mask``: uint8 or bool per token."""
+    d, T = _balance_desc(desc), int(T)
+    if T > 0 and topk_ids is None:
+        raise ValueError("topk_ids: required")
+    _need_tokens(d, logits, topk_ids, T, seq_off, mask)
+    _need_balance(d, out, ("counts", "tokens", "prob", "frac", "loss"))
+    _need(ws, "ws", torch.uint8, 0)
+    o = out.c()
+    st = _on(_device_of(out.loss, logits, topk_ids, seq_off, mask, out.counts, out.tokens, out.prob, out.frac, ws),
+             load().ft_balance_loss, ctypes.byref(d), _ptr(logits), _ptr(topk_ids), T, _ptr(seq_off), _ptr(mask),
+             ctypes.byref(o), _ptr(ws), ws.numel(), stream)
+    _check(st, "ft_balance_loss")
+
+
+def ft_router_backward(desc: dict, logits: torch.Tensor, topk_ids: Optional[torch.Tensor], T: int,
+                       balance: Optional[BalanceBuffers], d_loss: Optional[torch.Tensor], d_logits: torch.Tensor,
+                       topk_w: Optional[torch.Tensor] = None, d_topk_w: Optional[torch.Tensor] = None,
+                       seq_off: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None, stream=None) -> None:
+    """``balance`` and ``d_loss`` may be None (gates only), or ``d_topk_w`` (loss only)."""
+    d, T = _balance_desc(desc), int(T)
+    _need_tokens(d, logits, topk_ids, T, seq_off, mask)
+    if T == 0:
+        return
+    _need(d_logits, "d_logits", torch.float32, T * d.n_experts)
+    b, used = ft_balance_t(), ()
+    if d_loss is not None:
+        _need(d_loss, "d_loss", torch.float32, d.n_seq)
+        _need_balance(d, balance, ("tokens", "frac"))
+        used = (balance.tokens, balance.frac)
+        b.tokens, b.frac = map(_ptr, used)
+    if d_topk_w is not None:
+        if topk_ids is None:
+            raise ValueError("topk_ids: required with d_topk_w")
+        _need(topk_w, "topk_w", torch.float32, T * d.top_k)
+        _need(d_topk_w, "d_topk_w", torch.float32, T * d.top_k)
+    st = _on(_device_of(logits, topk_ids, d_logits, d_loss, topk_w, d_topk_w, seq_off, mask, *used),
+             load().ft_router_backward, ctypes.byref(d), _ptr(logits), _ptr(topk_ids), T, _ptr(seq_off), _ptr(mask),
+             ctypes.byref(b), _ptr(d_loss), _ptr(topk_w), _ptr(d_topk_w), _ptr(d_logits), stream)
+    _check(st, "ft_router_backward")

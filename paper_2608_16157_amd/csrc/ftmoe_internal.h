@@ -29,6 +29,48 @@ constexpr int kSkinnyRows = 64;         // most token rows of a skinny tile (ski
 constexpr int kSkinnyMinTokens = 4;     // fewest tokens of a call that takes skinny tiles (skinny_path)
 constexpr int kGemmMinTokens = 256;     // token count from which the matrix-core path's workspace and combine are used
 
+constexpr int pad128(int n) { return (n + 127) / 128 * 128; }
+
+// One 8-bit form (ft_act_codes_t) of R rows: codes [R][Kp], scale bytes [Kp / 128][Rp].
+struct ActForm {
+    uint8_t *codes;
+    uint8_t *scales;
+    int R, Kp, Rp;
+};
+
+// out [R][M] = B A^T over 8-bit operands with one scale per block of 128 (linear.hip).
+struct ProductArgs {
+    const uint8_t *a;    // [M][Kp] codes
+    const void *as;      // float32 [ceil(M / 128)][Kp / 128], or e8m0 bytes [Kp / 128][asr]
+    const uint8_t *b;    // [R][Kp] codes (null if x is given)
+    const uint8_t *bs;   // e8m0 bytes [Kp / 128][bsr]
+    const void *x;       // [R][K] bf16 or float32, quantised on the way
+    void *out;
+    int M, R, K, Kp, asr, bsr;
+};
+
+// Per-sequence balance statistics of the router (balance.hip).
+struct BalanceArgs {
+    const float *logits;       // [T][E]
+    const int32_t *topk_ids;   // [T][k]
+    const int32_t *seq_off;    // [n_seq + 1] or null (one sequence of T)
+    const uint8_t *mask;       // [T] or null
+    int T, E, k, gating, n_seq;
+    float coef;
+    int32_t *counts;           // [n_seq][E]
+    int32_t *tokens;           // [n_seq]
+    float *prob, *frac;        // [n_seq][E]
+    float *loss;               // [n_seq]
+    int parts, part_tokens;    // two-launch form: parts of part_tokens tokens
+    float *ws_prob;            // [parts + n_seq][E]
+    int32_t *ws_count;         // [parts + n_seq][E]
+    int32_t *ws_tokens;        // [parts + n_seq]
+    // backward
+    const float *topk_w, *d_topk_w;   // [T][k] or null
+    const float *d_loss;              // [n_seq] or null
+    float *d_logits;                  // [T][E]
+};
+
 struct HostMailbox;   // a worker pool's device <-> host mailbox (defined with CpuPool)
 
 // Routing outputs (the caller's ft_route_t, flattened).
@@ -340,5 +382,20 @@ hipError_t launch_skinny(const ExpertArgs &a, hipStream_t s, bool down);
 // bf16 (streaming path); h quantised in place (streaming path)
 hipError_t launch_act_quant_x(const ExpertArgs &a, hipStream_t s);
 hipError_t launch_act_quant_h(const ExpertArgs &a, hipStream_t s);
+
+hipError_t launch_act_quantize(const void *x, bool f32, int T, int C, const ActForm &row, const ActForm &col, hipStream_t s);
+hipError_t launch_swiglu_quantize(const void *gu, bool f32, int T, int I, const ActForm &h, const ActForm &saved,
+                                  hipStream_t s);
+hipError_t launch_swiglu_backward(const ActForm &saved, const void *dh, bool f32, int T, int I, const ActForm &drow,
+                                  const ActForm &dcol, const ActForm &hcol, hipStream_t s);
+hipError_t launch_weight_transpose(const uint8_t *w, const float *s, uint8_t *wt, float *st, int N, int K, hipStream_t stream);
+// bx: 0 B is codes, 1 x is bf16, 2 x is float32 (only up to kDirectTokens rows); out: 0 bf16, 1 float32, 2 added
+hipError_t launch_product(const ProductArgs &p, bool a_e8m0, int bx, int out, hipStream_t s);
+constexpr int kDirectTokens = 16;   // rows up to which a product quantises its input itself
+constexpr int kBalWholeTokens = 512;   // tokens up to which one launch sums each sequence in one workgroup
+constexpr int kBalMaxParts = 256;      // beyond: parts of the tokens, one workgroup each, and their join
+constexpr int kBalMinPart = 32;
+hipError_t launch_balance(const BalanceArgs &a, hipStream_t s);
+hipError_t launch_router_backward(const BalanceArgs &a, hipStream_t s);
 
 }  // namespace ftmoe
