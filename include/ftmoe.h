@@ -520,11 +520,12 @@ ft_status_t ft_act_quantize(const void *x, int32_t x_dtype, int32_t T, int32_t C
  *   y         [T][N] in y_dtype, overwritten.  FT_DT_BF16: fp8 matrix instructions, whose sums carry
  *             an error of about 2^-16 of the result, then one rounding to bf16.  FT_DT_F32:
  *             products and sums exact to float32's rounding, at half the matrix rate.
- *   ws        at least ft_linear_workspace_bytes(desc, T) bytes (FT_ERR_CAPACITY); none with
- *             FT_DT_FP8_ACT, where that is 0 and ws may be NULL
- * Sums run in a fixed order: results do not change between calls.  The gradient of x is the same
+ *   ws        at least ft_linear_workspace_bytes(desc, T) bytes (FT_ERR_CAPACITY): room for x's row
+ *             form and for the parts of a reduction that is split because the call has few rows.  With
+ *             FT_DT_FP8_ACT ws may be NULL: nothing is split then, slower for some tens to hundreds of rows
+ * Sums run in a fixed order: results do not change between equal calls.  The gradient of x is the same
  * product over the transposed weight: dx = ft_linear(out K, in N, w^T, dy).
- * ft_linear_workspace_bytes: bytes for up to max_tokens tokens; 0 too if desc is invalid.
+ * ft_linear_workspace_bytes: bytes for up to max_tokens tokens; 0 if desc is invalid.
  */
 typedef struct {
     int32_t out_features, in_features, x_dtype, y_dtype;

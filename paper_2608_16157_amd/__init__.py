@@ -780,12 +780,12 @@ def ft_linear_workspace_bytes(desc: dict, max_tokens: int) -> int:
     return int(load().ft_linear_workspace_bytes(ctypes.byref(_linear_desc(desc)), int(max_tokens)))
 
 
-def alloc_linear_workspace(desc: dict, max_tokens: int, device="cuda") -> Optional[torch.Tensor]:
-    """Workspace of ft_linear for up to max_tokens tokens; None where the call needs none."""
+def alloc_linear_workspace(desc: dict, max_tokens: int, device="cuda") -> torch.Tensor:
+    """Workspace of ft_linear for up to max_tokens tokens."""
     n = ft_linear_workspace_bytes(desc, max_tokens)
-    if n == 0 and int(desc["x_dtype"]) != FT_DT_FP8_ACT:
+    if n == 0:
         raise FtError(FT_ERR_SHAPE, "ft_linear_workspace_bytes")
-    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+    return torch.empty(n, dtype=torch.uint8, device=device)
 
 
 def _need_weight(weight: dict, name: str, N: int, K: int) -> None:
@@ -797,7 +797,7 @@ def _need_weight(weight: dict, name: str, N: int, K: int) -> None:
 def ft_linear(desc: dict, weight: dict, x, T: int, y: torch.Tensor, ws: Optional[torch.Tensor] = None,
               stream=None) -> None:
     """``x``: a device tensor [T][in_features] of x_dtype, or with FT_DT_FP8_ACT its row form
-    (ActCodes)."""
+    (ActCodes); ``ws`` may be None with the latter only."""
     d, T = _linear_desc(desc), int(T)
     N, K = d.out_features, d.in_features
     _need_sizes(T, N, K)
@@ -807,6 +807,8 @@ def ft_linear(desc: dict, weight: dict, x, T: int, y: torch.Tensor, ws: Optional
     if d.x_dtype == FT_DT_FP8_ACT:
         _need_codes(x, "x", T, K)
         xp, xs = x.codes, x.scales
+        if ws is not None:
+            _need(ws, "ws", torch.uint8, 0)
     else:
         if d.x_dtype not in _X_DTYPES:
             raise FtError(FT_ERR_DTYPE, "ft_linear")

@@ -40,6 +40,22 @@ ft_status_t linear_status(const ft_linear_desc_t *d) {
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
+// ft_linear's workspace: the row form of x, and the parts of a split reduction (product_plan holds their
+// bytes to kSplitBytes, and to kMaxParts outputs).  Grows with T.
+struct LinearWs {
+    size_t codes, scales, parts, total;
+};
+LinearWs linear_ws(const ft_linear_desc_t *d, int T) {
+    const size_t Kp = pad128(d->in_features), Tp = pad128(std::max(T, 1));
+    const bool packed = d->x_dtype == FT_DT_FP8_ACT;
+    LinearWs w;
+    w.codes = 0;
+    w.scales = packed ? 0 : Tp * Kp;
+    w.parts = w.scales + (packed ? 0 : round256(Tp * (Kp / 128)));
+    w.total = w.parts + std::min(kSplitBytes, round256(static_cast<size_t>(kMaxParts) * std::max(T, 1) * d->out_features * 4));
+    return w;
+}
+
 ft_status_t balance_status(const ft_balance_desc_t *d) {
     if (!d) return FT_ERR_NULL;
     if (d->n_experts < 1 || d->n_experts > kMaxExperts || d->top_k < 1 || d->top_k > d->n_experts || d->top_k > kMaxTopK)
@@ -107,9 +123,8 @@ ft_status_t ft_act_quantize(const void *x, int32_t x_dtype, int32_t T, int32_t C
 
 size_t ft_linear_workspace_bytes(const ft_linear_desc_t *desc, int32_t max_tokens) {
     if (linear_status(desc) != FT_OK || !tokens_ok(max_tokens)) return 0;
-    if (desc->x_dtype == FT_DT_FP8_ACT) return 0;
-    const size_t Kp = pad128(desc->in_features), Tp = pad128(std::max(max_tokens, 1));
-    return round256(Tp * Kp) + round256(Tp * (Kp / 128));
+    const LinearWs w = linear_ws(desc, max_tokens);
+    return w.total;
 }
 
 ft_status_t ft_linear(const ft_linear_desc_t *desc, const uint8_t *w, const float *w_scales, const void *x,
@@ -118,11 +133,14 @@ ft_status_t ft_linear(const ft_linear_desc_t *desc, const uint8_t *w, const floa
     if (!tokens_ok(T)) return FT_ERR_SHAPE;
     if (T == 0) return FT_OK;
     const bool packed = desc->x_dtype == FT_DT_FP8_ACT;
-    if (!w || !w_scales || !x || !y || (packed && !x_scales)) return FT_ERR_NULL;
-    if (!aligned(w) || !aligned(x) || !aligned(y) || (packed && !aligned(x_scales)) ||
+    if (!w || !w_scales || !x || !y || (packed && !x_scales) || (!packed && !ws)) return FT_ERR_NULL;
+    const LinearWs L = linear_ws(desc, T);
+    if (ws && ws_bytes < L.total) return FT_ERR_CAPACITY;
+    if (!aligned(w) || !aligned(x) || !aligned(y) || (packed && !aligned(x_scales)) || !aligned(ws) ||
         reinterpret_cast<uintptr_t>(w_scales) % 4)
         return FT_ERR_SHAPE;
     const hipStream_t s = static_cast<hipStream_t>(stream);
+    uint8_t *base = static_cast<uint8_t *>(ws);
     ProductArgs p{};
     p.a = w;
     p.as = w_scales;
@@ -136,24 +154,18 @@ ft_status_t ft_linear(const ft_linear_desc_t *desc, const uint8_t *w, const floa
     if (packed) {
         p.b = static_cast<const uint8_t *>(x);
         p.bs = x_scales;
+    } else if (T <= kDirectTokens) {
+        p.x = x;
+        bx = desc->x_dtype == FT_DT_BF16 ? 1 : 2;
     } else {
-        const size_t need = ft_linear_workspace_bytes(desc, T);
-        if (!ws) return FT_ERR_NULL;
-        if (ws_bytes < need) return FT_ERR_CAPACITY;
-        if (!aligned(ws)) return FT_ERR_SHAPE;
-        if (T <= kDirectTokens) {
-            p.x = x;
-            bx = desc->x_dtype == FT_DT_BF16 ? 1 : 2;
-        } else {
-            uint8_t *codes = static_cast<uint8_t *>(ws);
-            const ft_act_codes_t q{codes, codes + round256(static_cast<size_t>(p.bsr) * p.Kp)};
-            if (launch_act_quantize(x, desc->x_dtype == FT_DT_F32, T, p.K, form(&q, T, p.K), ActForm{}, s) != hipSuccess)
-                return FT_ERR_HIP;
-            p.b = q.codes;
-            p.bs = q.scales;
-        }
+        const ft_act_codes_t q{base + L.codes, base + L.scales};
+        if (launch_act_quantize(x, desc->x_dtype == FT_DT_F32, T, p.K, form(&q, T, p.K), ActForm{}, s) != hipSuccess)
+            return FT_ERR_HIP;
+        p.b = q.codes;
+        p.bs = q.scales;
     }
-    return launch_product(p, false, bx, desc->y_dtype == FT_DT_F32 ? 1 : 0, s) == hipSuccess ? FT_OK : FT_ERR_HIP;
+    float *parts = ws ? reinterpret_cast<float *>(base + L.parts) : nullptr;
+    return launch_product(p, false, bx, desc->y_dtype == FT_DT_F32 ? 1 : 0, parts, s) == hipSuccess ? FT_OK : FT_ERR_HIP;
 }
 
 ft_status_t ft_linear_transpose(int32_t out_features, int32_t in_features, const uint8_t *w, const float *w_scales,
@@ -194,7 +206,7 @@ ft_status_t ft_linear_weight_grad(int32_t out_features, int32_t in_features, int
     p.asr = pad128(in_features);
     p.bsr = pad128(out_features);
     const int out = dw_dtype == FT_DT_BF16 ? 0 : accumulate ? 2 : 1;
-    return launch_product(p, true, 0, out, static_cast<hipStream_t>(stream)) == hipSuccess ? FT_OK : FT_ERR_HIP;
+    return launch_product(p, true, 0, out, nullptr, static_cast<hipStream_t>(stream)) == hipSuccess ? FT_OK : FT_ERR_HIP;
 }
 
 ft_status_t ft_swiglu_quantize(const void *gu, int32_t gu_dtype, int32_t T, int32_t inter, const ft_act_codes_t *h,

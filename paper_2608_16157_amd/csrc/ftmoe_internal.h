@@ -46,8 +46,19 @@ struct ProductArgs {
     const uint8_t *bs;   // e8m0 bytes [Kp / 128][bsr]
     const void *x;       // [R][K] bf16 or float32, quantised on the way
     void *out;
+    float *part;         // split reduction: [parts][R][M] float32 sums (null: out is written)
     int M, R, K, Kp, asr, bsr;
 };
+
+// How a product runs: which kernel, and into how many parts its reduction is split.
+struct ProductPlan {
+    enum Kernel { kDirect16, kDirect32, kDirect64, kDirect128, kTile64, kTile128, kTile256 };
+    Kernel kernel;
+    int parts;
+};
+constexpr int kMaxParts = 16;
+constexpr size_t kSplitBytes = 32u << 20;   // most bytes of the parts of a split reduction
+ProductPlan product_plan(int M, int R, int Kp, bool wide, bool may_split);
 
 // Per-sequence balance statistics of the router (balance.hip).
 struct BalanceArgs {
@@ -390,7 +401,8 @@ hipError_t launch_swiglu_backward(const ActForm &saved, const void *dh, bool f32
                                   const ActForm &dcol, const ActForm &hcol, hipStream_t s);
 hipError_t launch_weight_transpose(const uint8_t *w, const float *s, uint8_t *wt, float *st, int N, int K, hipStream_t stream);
 // bx: 0 B is codes, 1 x is bf16, 2 x is float32 (only up to kDirectTokens rows); out: 0 bf16, 1 float32, 2 added
-hipError_t launch_product(const ProductArgs &p, bool a_e8m0, int bx, int out, hipStream_t s);
+// ws: room for the parts of a split reduction, or null
+hipError_t launch_product(const ProductArgs &p, bool a_e8m0, int bx, int out, float *ws, hipStream_t s);
 constexpr int kDirectTokens = 16;   // rows up to which a product quantises its input itself
 constexpr int kBalWholeTokens = 512;   // tokens up to which one launch sums each sequence in one workgroup
 constexpr int kBalMaxParts = 256;      // beyond: parts of the tokens, one workgroup each, and their join

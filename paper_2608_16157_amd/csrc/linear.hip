@@ -15,18 +15,21 @@
 // scale multiplies the finished float32 sum of its block in either case.
 #include "act_codes.h"
 #include "ftmoe_internal.h"
+#include "gemm_tile.h"
 
+#include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 namespace ftmoe {
 
 __device__ __forceinline__ i32x8_vec_t codes32(const uint8_t *p) {
-    const uint4 lo = reinterpret_cast<const uint4 *>(p)[0], hi = reinterpret_cast<const uint4 *>(p)[1];
+    const uint4 lo = reinterpret_cast<const uint4 *>(p)[0], hi = reinterpret_cast<const uint4 *>(p)[4];
     return i32x8_vec_t{static_cast<int>(lo.x), static_cast<int>(lo.y), static_cast<int>(lo.z), static_cast<int>(lo.w),
                        static_cast<int>(hi.x), static_cast<int>(hi.y), static_cast<int>(hi.z), static_cast<int>(hi.w)};
 }
 
-// four consecutive results: bf16 (rounded once, to nearest even), float32, or added to the float32 there
+// four consecutive results: 0 bf16 (rounded once, to nearest even), 1 float32, 2 added to the float32 there
 template <int OUT>
 __device__ __forceinline__ void store4(void *out, size_t at, floatx4_t v) {
     if constexpr (OUT == 0) {
@@ -38,14 +41,33 @@ __device__ __forceinline__ void store4(void *out, size_t at, floatx4_t v) {
     }
 }
 
+// The reduction may be split over the grid's third dimension: each part sums its blocks into float32 rows of
+// its own in the workspace (p.part), which product_join adds in order.
+__device__ __forceinline__ void split_range(const ProductArgs &p, int nkb, int &kb0, int &kb1) {
+    kb0 = static_cast<int>(static_cast<long>(nkb) * blockIdx.z / gridDim.z);
+    kb1 = static_cast<int>(static_cast<long>(nkb) * (blockIdx.z + 1) / gridDim.z);
+}
+__device__ __forceinline__ void *split_out(const ProductArgs &p) {
+    return p.part ? p.part + static_cast<size_t>(blockIdx.z) * p.R * p.M : p.out;
+}
+
+template <int OUT>
+__global__ __launch_bounds__(256) void product_join(ProductArgs p, int parts) {
+    const size_t n = static_cast<size_t>(p.R) * p.M, i = (static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
+    if (i >= n) return;
+    floatx4_t v = *reinterpret_cast<const floatx4_t *>(p.part + i);
+    for (int z = 1; z < parts; ++z) v += *reinterpret_cast<const floatx4_t *>(p.part + z * n + i);
+    store4<OUT>(p.out, i, v);
+}
+
 // Direct kernel: operands from global memory to registers, the reduction split over the waves of a
 // workgroup and joined in LDS in a fixed order.  A wave holds 16 RA rows of A and 16 TB rows of B; lane
 // (r = lane % 16, g = lane / 16) the 32 codes [32 g, 32 g + 32) of row r of a block.
 // BX: 0 B is codes; 1 B is bf16, 2 float32, quantised on the way.  ASC: 0 float32 block scales, 1 e8m0.
-// OUT: 0 bf16, 1 float32, 2 float32 added to what is there.
-template <int RA, int TB, int W, int ASC, int BX, int OUT>
+// WIDE: the arithmetic of float32 results.  OUT: see store4.
+template <int RA, int TB, int W, int ASC, int BX, bool WIDE, int OUT>
 __global__ __launch_bounds__(64 * W) void product_direct(ProductArgs p) {
-    constexpr bool kWide = OUT != 0;
+    constexpr bool kWide = WIDE;
     constexpr int kTile = RA * TB * 256;
     __shared__ float red[W / 2][kTile];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = lane_id();
@@ -59,12 +81,14 @@ __global__ __launch_bounds__(64 * W) void product_direct(ProductArgs p) {
         for (int j = 0; j < TB; ++j) acc[i][j] = floatx4_t{};
     const uint8_t *ap[RA];
 #pragma unroll
-    for (int i = 0; i < RA; ++i) ap[i] = p.a + static_cast<size_t>(min(a0 + 16 * i + r, p.M - 1)) * p.Kp + 32 * g;
+    for (int i = 0; i < RA; ++i) ap[i] = p.a + static_cast<size_t>(min(a0 + 16 * i + r, p.M - 1)) * p.Kp + 16 * g;
     int brow[TB];
 #pragma unroll
     for (int j = 0; j < TB; ++j) brow[j] = min(b0 + 16 * j + r, p.R - 1);
 
-    for (int kb = wave; kb < nkb; kb += W) {
+    int kb0, kb1;
+    split_range(p, nkb, kb0, kb1);
+    for (int kb = kb0 + wave; kb < kb1; kb += W) {
         i32x8_vec_t a[RA], b[TB];
         int sb[TB];
 #pragma unroll
@@ -72,7 +96,7 @@ __global__ __launch_bounds__(64 * W) void product_direct(ProductArgs p) {
 #pragma unroll
         for (int j = 0; j < TB; ++j) {
             if constexpr (BX == 0) {
-                b[j] = codes32(p.b + static_cast<size_t>(brow[j]) * p.Kp + static_cast<size_t>(kb) * 128 + 32 * g);
+                b[j] = codes32(p.b + static_cast<size_t>(brow[j]) * p.Kp + static_cast<size_t>(kb) * 128 + 16 * g);
                 sb[j] = p.bs[static_cast<size_t>(kb) * p.bsr + brow[j]];
             } else {
                 using XT = std::conditional_t<BX == 1, uint16_t, float>;
@@ -80,7 +104,7 @@ __global__ __launch_bounds__(64 * W) void product_direct(ProductArgs p) {
                 float v[32];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int k = kb * 128 + 32 * g + 8 * q;
+                    const int k = kb * 128 + q / 2 * 64 + 16 * g + q % 2 * 8;
                     if (k < p.K) load8(x + k, v + 8 * q);   // K is a multiple of 16
                     else
 #pragma unroll
@@ -149,7 +173,234 @@ __global__ __launch_bounds__(64 * W) void product_direct(ProductArgs p) {
 #pragma unroll
         for (int i = 0; i < RA; ++i) {
             const int a = a0 + 16 * i + 4 * g;
-            if (a < p.M) store4<OUT>(p.out, static_cast<size_t>(b) * p.M + a, acc[i][j]);   // M is a multiple of 16
+            if (a < p.M) store4<OUT>(split_out(p), static_cast<size_t>(b) * p.M + a, acc[i][j]);   // M is a multiple of 16
+        }
+    }
+}
+
+// Tiled kernel: a workgroup of GA x GB waves owns a tile of 16 WA GA rows of A by 16 WB GB rows of B, each
+// wave 16 WA x 16 WB of it.  Blocks (128 codes of every row of both operands, and their e8m0 bytes) go from
+// global memory straight into LDS; 16-byte chunks lie XOR-swizzled by their row, so that the operand
+// reads of 16 consecutive rows meet no bank twice.  A wave keeps the block's B operands in registers and
+// walks the A operands, one per step: each step reads the next A operand while the matrix instructions of
+// the current one run, and the float32 scale of the sums before is applied between them.
+//
+// What bounds it is how fast L2 fills LDS, and that is a matter of bytes in flight.  B's place in LDS is
+// free as soon as the block's operands are in registers, A's half by half, so B lies in a ring of two
+// blocks and A in one of five half blocks, and everything is requested about two blocks before it is
+// read.  The two hand-offs of a block, in the last step of each half: wait for what the next step reads
+// (requests return in order, so the younger ones may stay in flight) and for this wave's own LDS reads,
+// barrier, and request into the freed places between the step's matrix instructions.
+template <int WA, int WB, int GA, int GB, int ASC, bool WIDE, int OUT>
+__global__ __launch_bounds__(64 * GA * GB, 2) void product_tiled(ProductArgs p, int na, int nb) {
+    constexpr bool kWide = WIDE;
+    constexpr int NW = GA * GB, BA = 16 * WA * GA, BB = 16 * WB * GB, HS = WA / 2;   // HS steps per half
+    constexpr int kHalf = BA / 2 * 128, kAHalves = 5, kBBlock = BB * 128;
+    constexpr int kB = kAHalves * kHalf, kS = kB + 2 * kBBlock;     // LDS: A halves, B blocks, 4 blocks' scales
+    constexpr int AH = BA / 2 / 8 / NW, BI = BB / 8 / NW;           // 1 KB requests per wave
+    constexpr int kInFlight = 3 * AH + BI + 1;                      // younger than what a hand-off waits for
+    static_assert(AH * 16 * NW == BA && BI * 8 * NW == BB && BA <= 256 && BB <= 256 && WA % 2 == 0, "tile");
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[kS + 4 * 512];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = lane_id();
+    const int r = lane & 15, g = lane >> 4, wa = wave % GA, wb = wave / GA;
+    // tiles that run at the same time on one XCD form a patch of kBand B tiles by some A tiles
+    constexpr int kBand = 4;
+    const int L = xcd_remap(blockIdx.x, na * nb);
+    const int band = L / (kBand * na), rem = L - band * (kBand * na);
+    const int bw = min(kBand, nb - band * kBand);
+    const int a0 = rem / bw * BA, b0 = (band * kBand + rem % bw) * BB;
+    int k0, k1;
+    split_range(p, p.Kp / 128, k0, k1);
+    const int nkb = k1 - k0;   // blocks k0 .. k0 + nkb - 1 of the Kp / 128
+
+    // requests: lane i of one fills 16 bytes of row i / 8 of its 8 rows, the chunk that belongs at place
+    // i % 8.  Half H of an A block holds the rows of the steps [H HS, (H + 1) HS), 16 HS of each GA.
+    const uint8_t *abase = p.a + static_cast<size_t>(a0) * p.Kp + static_cast<size_t>(k0) * 128;
+    const uint8_t *bbase = p.b + static_cast<size_t>(b0) * p.Kp + static_cast<size_t>(k0) * 128;
+    uint32_t aoff[2][AH], boff[BI];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < AH; ++i) {
+            const int at = (wave * AH + i) * 8 + lane / 8;   // row of the half
+            const int row = at / (16 * HS) * (16 * WA) + h * 16 * HS + at % (16 * HS);
+            aoff[h][i] = static_cast<uint32_t>(min(row, p.M - 1 - a0)) * p.Kp + (swz<128>(at, lane % 8) << 4);
+        }
+#pragma unroll
+    for (int i = 0; i < BI; ++i) {
+        const int row = (wave * BI + i) * 8 + lane / 8;
+        boff[i] = static_cast<uint32_t>(min(row, p.R - 1 - b0)) * p.Kp + (swz<128>(row, lane % 8) << 4);
+    }
+    // scales of a block: B's e8m0 bytes, and, asked for by the odd waves, A's, or the float32 scales of the
+    // tile's one or two weight blocks (32 copies each: every lane of a request brings one word).  Every
+    // wave asks, the same words to the same place: a branch here would split the loop's body, which the
+    // compiler then reorders.
+    const bool sa_wave = wave & 1;
+    const size_t srow = sa_wave ? (ASC ? p.asr : 4) : p.bsr;
+    const uint8_t *sbase = (sa_wave ? static_cast<const uint8_t *>(p.as) : p.bs) + k0 * srow;
+    const int sdst = sa_wave ? 256 : 0;
+    const uint32_t soff = !sa_wave ? min(b0 + 4 * lane, p.bsr - 4)
+                          : ASC    ? min(a0 + 4 * lane, p.asr - 4)
+                                   : static_cast<uint32_t>(min(a0 / 128 + lane / 32, (p.M - 1) / 128)) * (p.Kp / 128) * 4;
+    const uint32_t l0 = lds_address(lds);
+    // past the last block the requests repeat it
+    auto request_a = [&](auto half, auto i, int kb, int slot) {
+        constexpr int H = decltype(half)::value, I = decltype(i)::value;
+        dma16(abase + static_cast<size_t>(min(kb, nkb - 1)) * 128, aoff[H][I], l0 + slot + (wave * AH + I) * 1024);
+    };
+    auto request_b = [&](auto i, int kb) {
+        constexpr int I = decltype(i)::value;
+        const int k = min(kb, nkb - 1);
+        if constexpr (I < BI) dma16(bbase + static_cast<size_t>(k) * 128, boff[I], l0 + kB + (kb & 1) * kBBlock + (wave * BI + I) * 1024);
+        else dma4(sbase + static_cast<size_t>(k) * srow, soff, l0 + kS + (kb & 3) * 512 + sdst);
+    };
+    // operand reads: chunks g and g + 4 of row r of a 16-row tile (which codes of the block a lane holds is free
+    // as long as A and B agree).  Chunks 2 g and 2 g + 1 would meet banks twice: 123 against 221 B/clk.
+    const int chunk = swz<128>(r, g) << 4, other = (chunk ^ 64) - chunk;
+    const uint8_t *la = lds + (wa * HS * 16 + r) * 128 + chunk, *lb = lds + kB + (wb * WB * 16 + r) * 128 + chunk;
+    const uint8_t *lbs = lds + kS + wb * WB * 16 + r, *las = lds + kS + 256 + wa * WA * 16 + r;
+    auto operand = [&](const uint8_t *q) {
+        const u32x4_t lo = *reinterpret_cast<const u32x4_t *>(q), hi = *reinterpret_cast<const u32x4_t *>(q + other);
+        return i32x8_vec_t{static_cast<int>(lo[0]), static_cast<int>(lo[1]), static_cast<int>(lo[2]), static_cast<int>(lo[3]),
+                           static_cast<int>(hi[0]), static_cast<int>(hi[1]), static_cast<int>(hi[2]), static_cast<int>(hi[3])};
+    };
+    const uint8_t *lws = lds + kS + 256 + wa * WA * 16 / 128 * 128;
+    auto weight_scale = [&](int slot) { return ASC ? 1.0f : *reinterpret_cast<const float *>(lws + slot); };
+
+    constexpr int kLag = WB;   // sums in flight between a matrix instruction and its scale
+    floatx4_t acc[WA][WB], z[kLag];
+#pragma unroll
+    for (int i = 0; i < WA; ++i)
+#pragma unroll
+        for (int j = 0; j < WB; ++j) acc[i][j] = floatx4_t{};
+#pragma unroll
+    for (int j = 0; j < kLag; ++j) z[j] = floatx4_t{};
+    i32x8_vec_t a, b[WB];
+    int sa = 127, sb[WB];
+    bf16x8_t bwide[kWide ? WB : 1][4];
+
+    auto all_a = [&](auto half, int kb, int slot) { static_for<0, AH>([&](auto i) { request_a(half, i, kb, slot); }); };
+    auto all_b = [&](int kb) { static_for<0, BI + 1>([&](auto i) { request_b(i, kb); }); };
+    all_a(ic<0>{}, 0, 0);
+    all_b(0);
+    all_a(ic<1>{}, 0, kHalf);
+    all_a(ic<0>{}, 1, 2 * kHalf);
+    all_b(1);
+    all_a(ic<1>{}, 1, 3 * kHalf);
+    all_a(ic<0>{}, 2, 4 * kHalf);
+    wait_vmcnt<4 * AH + BI + 1>();
+    stage_barrier();
+    a = operand(la);
+    if (ASC) sa = las[0];
+#pragma unroll
+    for (int j = 0; j < WB; ++j) {
+        b[j] = operand(lb + j * 2048);
+        sb[j] = lbs[16 * j];
+    }
+    float sw = weight_scale(0), swz_old = 0.0f;   // weight scale of this block, and of the sums in z
+    int s0 = 0;                                   // A slot of the block's first half
+    auto after = [&](int slot) { return slot + kHalf == kAHalves * kHalf ? 0 : slot + kHalf; };
+    for (int kb = 0; kb < nkb; ++kb) {
+        const int s1 = after(s0), s2 = after(s1), bn = ((kb + 1) & 1) * kBBlock, sn = ((kb + 1) & 3) * 512;
+        float sw_next = sw;
+        if constexpr (kWide)
+#pragma unroll
+            for (int j = 0; j < WB; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) bwide[j][q] = act_bf16x8(b[j][2 * q], b[j][2 * q + 1], act_scale_operand(sb[j]));
+        static_for<0, WA>([&](auto ii) {
+            constexpr int I = decltype(ii)::value, P = (I + WA - 1) % WA, N = (I + 1) % WA;
+            constexpr bool kMid = I == HS - 1, kLast = I == WA - 1;
+            if constexpr (kMid || kLast) {
+                wait_vmcnt<kInFlight>();
+                wait_lgkmcnt0();
+                stage_barrier();
+            }
+            // requests number Q of the step's WB groups
+            auto requests = [&](auto qq) {
+                constexpr int Q = decltype(qq)::value;
+                if constexpr (kMid) {
+                    static_for<Q * (BI + 1) / WB, (Q + 1) * (BI + 1) / WB>([&](auto i) { request_b(i, kb + 2); });
+                    if constexpr (Q == WB - 1) all_a(ic<1>{}, kb + 2, s0);
+                }
+                if constexpr (kLast && Q == 0) all_a(ic<0>{}, kb + 3, s1);
+            };
+            if constexpr (kWide) static_for<0, WB>(requests);
+            const i32x8_vec_t an = operand(la + (kLast ? s2 : N < HS ? s0 : s1) + N % HS * 2048);
+            if constexpr (kLast) sw_next = weight_scale(sn);
+            const int san = ASC ? las[kLast ? sn : (kb & 3) * 512 + N * 16] : 127;
+            if constexpr (kWide) {
+                floatx4_t zn[WB];
+#pragma unroll
+                for (int j = 0; j < WB; ++j) zn[j] = ASC ? acc[I][j] : floatx4_t{};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const bf16x8_t aw = act_bf16x8(a[2 * q], a[2 * q + 1], act_scale_operand(sa));
+#pragma unroll
+                    for (int j = 0; j < WB; ++j) zn[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(aw, bwide[j][q], zn[j], 0, 0, 0);
+                }
+                if constexpr (kLast) {
+#pragma unroll
+                    for (int j = 0; j < WB; ++j) {
+                        b[j] = operand(lb + bn + j * 2048);
+                        sb[j] = lbs[sn + 16 * j];
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < WB; ++j) {
+                    if constexpr (ASC) {
+                        acc[I][j] = zn[j];
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) acc[P][j][q] = fmaf(I == 0 ? swz_old : sw, z[j][q], acc[P][j][q]);
+                        z[j] = zn[j];
+                    }
+                }
+            } else {
+                // in program order: one matrix instruction, the scale of the sums kLag instructions back, and
+                // in the last step the next block's operand into the registers the instruction has just read
+                __builtin_amdgcn_sched_barrier(0);
+                static_for<0, WB>([&](auto jj) {
+                    constexpr int J = decltype(jj)::value;
+                    if constexpr (ASC) {
+                        acc[I][J] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b[J], acc[I][J], 0, 0, 0, sa, 0, sb[J]);
+                    } else {
+                        constexpr int T = I * WB + J, F = (T + WA * WB - kLag) % (WA * WB);
+                        const float f = T < kLag ? swz_old : sw;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            acc[F / WB][F % WB][q] = fmaf(f, z[F % kLag][q], acc[F / WB][F % WB][q]);
+                        z[T % kLag] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b[J], floatx4_t{}, 0, 0, 0, sa, 0, sb[J]);
+                    }
+                    requests(jj);
+                    if constexpr (kLast) {
+                        b[J] = operand(lb + bn + J * 2048);
+                        sb[J] = lbs[sn + 16 * J];
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            }
+            a = an;
+            sa = san;
+        });
+        swz_old = sw;
+        sw = sw_next;
+        s0 = s2;
+    }
+    wait_vmcnt<0>();   // the requests past the end
+    if constexpr (!ASC)
+#pragma unroll
+        for (int j = 0; j < WB; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) acc[WA - 1][j][q] = fmaf(swz_old, z[j][q], acc[WA - 1][j][q]);
+#pragma unroll
+    for (int j = 0; j < WB; ++j) {
+        const int bi = b0 + (wb * WB + j) * 16 + r;
+        if (bi >= p.R) continue;
+#pragma unroll
+        for (int i = 0; i < WA; ++i) {
+            const int ai = a0 + (wa * WA + i) * 16 + 4 * g;
+            if (ai < p.M) store4<OUT>(split_out(p), static_cast<size_t>(bi) * p.M + ai, acc[i][j]);
         }
     }
 }
@@ -194,25 +445,120 @@ hipError_t launch_weight_transpose(const uint8_t *w, const float *s, uint8_t *wt
     return hipGetLastError();
 }
 
-template <int ASC, int BX, int OUT>
-static hipError_t direct(const ProductArgs &p, hipStream_t s) {
-    if (p.R <= 16) {
-        hipLaunchKernelGGL((product_direct<1, 1, 8, ASC, BX, OUT>), dim3((p.M + 15) / 16, 1), dim3(512), 0, s, p);
-    } else if constexpr (BX == 0) {
-        hipLaunchKernelGGL((product_direct<4, 4, 4, ASC, BX, OUT>), dim3((p.M + 63) / 64, (p.R + 63) / 64), dim3(256), 0, s, p);
+template <int WA, int WB, int GA, int GB, int ASC, bool WIDE, int OUT>
+static void tiled(const ProductArgs &p, int parts, hipStream_t s) {
+    const int na = (p.M + 16 * WA * GA - 1) / (16 * WA * GA), nb = (p.R + 16 * WB * GB - 1) / (16 * WB * GB);
+    hipLaunchKernelGGL((product_tiled<WA, WB, GA, GB, ASC, WIDE, OUT>), dim3(na * nb, 1, parts), dim3(64 * GA * GB), 0, s, p, na, nb);
+}
+
+template <int RA, int TB, int W, int ASC, int BX, bool WIDE, int OUT>
+static void direct(const ProductArgs &p, int parts, hipStream_t s) {
+    hipLaunchKernelGGL((product_direct<RA, TB, W, ASC, BX, WIDE, OUT>),
+                       dim3((p.M + 16 * RA - 1) / (16 * RA), (p.R + 16 * TB - 1) / (16 * TB), parts), dim3(64 * W), 0, s, p);
+}
+
+template <int ASC, int BX, bool WIDE, int OUT>
+static void variant(const ProductArgs &p, const ProductPlan &plan, hipStream_t s) {
+    if constexpr (BX != 0) {
+        direct<1, 1, 8, ASC, BX, WIDE, OUT>(p, 1, s);
+    } else {
+        switch (plan.kernel) {
+            case ProductPlan::kDirect16: direct<1, 1, 8, ASC, BX, WIDE, OUT>(p, plan.parts, s); break;
+            case ProductPlan::kDirect32: direct<1, 2, 8, ASC, BX, WIDE, OUT>(p, plan.parts, s); break;
+            case ProductPlan::kDirect64: direct<2, 2, 8, ASC, BX, WIDE, OUT>(p, plan.parts, s); break;
+            case ProductPlan::kDirect128: direct<2, 4, 8, ASC, BX, WIDE, OUT>(p, plan.parts, s); break;
+            case ProductPlan::kTile64: direct<4, 4, 4, ASC, BX, WIDE, OUT>(p, plan.parts, s); break;
+            case ProductPlan::kTile128: tiled<4, 4, 2, 2, ASC, WIDE, OUT>(p, plan.parts, s); break;
+            case ProductPlan::kTile256:
+                if constexpr (!WIDE) tiled<8, 4, 2, 4, ASC, WIDE, OUT>(p, plan.parts, s);
+                break;
+        }
+    }
+}
+
+// Which kernel runs a product, and into how many parts its reduction is split: the least of their estimated
+// times.  The estimate is a workgroup's blocks times what one takes (in microseconds, measured on this
+// card over N from 512 to 7168, K from 768 to 16384 and 16 to 8192 rows), as often as its workgroups
+// outnumber the 256 CUs, plus each round's start and end, plus the join of the parts:
+//   direct kernels  the bytes of a block at 34.5 GB/s a CU (the waves of a CU share that rate), at least
+//                   0.7 for every 8 blocks: a small reduction is one round trip to memory
+//   64 x 64         0.58 a block alone on its CU, 0.61 shared, whatever the arithmetic
+//   128 x 128       0.55 alone, 0.60 shared by two; widened 1.05 and 0.95
+//   256 x 256       1.63 rising to 1.9 when every CU has one
+// With M = 4096, K = 7168 (estimate / measured): 32 rows 12.9 / 12.7 (2 parts of 32 x 32 tiles), unsplit
+// 13.1 / 12.9 (16 x 32); 256 rows 20 / 20.4 (128 x 128, 4 parts), unsplit 35 / 34; 777 rows 35 / 38,
+// 2 parts 43 / 44; 4096 rows 115 / 110 (256 x 256), 138 / 136 (128 x 128).
+ProductPlan product_plan(int M, int R, int Kp, bool wide, bool may_split) {
+    struct Kind {
+        ProductPlan::Kernel kernel;
+        int a, b, most_rows;   // tile; rows up to which it is looked at
+        float ends;            // direct kernels: their start, and the join of the waves
+    };
+    static constexpr Kind kinds[] = {{ProductPlan::kDirect16, 16, 16, 32, 3.0f},   {ProductPlan::kDirect32, 16, 32, 64, 3.2f},
+                                     {ProductPlan::kDirect64, 32, 32, 256, 3.6f},  {ProductPlan::kDirect128, 32, 64, 512, 5.0f},
+                                     {ProductPlan::kTile64, 64, 64, 1024, 0},      {ProductPlan::kTile128, 128, 128, 1 << 30, 0},
+                                     {ProductPlan::kTile256, 256, 256, 1 << 30, 0}};
+    const int nkb = Kp / 128;
+    if (nkb == 0) return {ProductPlan::kTile64, 1};   // no block: zeros are stored
+    ProductPlan best{ProductPlan::kTile128, 1};
+    float least = 1e30f;
+    for (const Kind &k : kinds) {
+        if (R > k.most_rows || (k.kernel == ProductPlan::kTile256 && wide)) continue;
+        const float wgs = static_cast<float>((M + k.a - 1) / k.a) * static_cast<float>((R + k.b - 1) / k.b);
+        for (int parts = 1; parts <= kMaxParts && parts <= nkb; ++parts) {
+            if (parts > 1 && (!may_split || static_cast<size_t>(parts) * R * M * 4 > kSplitBytes)) break;
+            const int blocks = (nkb + parts - 1) / parts;
+            // workgroups of the fullest CU; behind the second round they even out
+            const float mean = wgs * parts / 256.0f, cu = mean > 2 ? mean + 0.25f : std::ceil(mean);
+            float t;
+            if (k.kernel == ProductPlan::kTile256) {
+                const float full = std::min(mean, 1.0f);
+                t = std::ceil(mean) * (blocks * (1.63f + 0.27f * full) + 4.0f + 4.0f * full);
+            } else if (k.kernel == ProductPlan::kTile128) {
+                t = blocks * (wide ? std::max(1.05f, 0.95f * cu) : std::max(0.55f, 0.60f * cu)) + 4.0f * std::ceil(cu / 2);
+            } else if (k.kernel == ProductPlan::kTile64) {
+                t = blocks * (cu <= 1 ? 0.58f : 0.61f * cu) + 4.5f;
+            } else {
+                t = std::max(cu * blocks * ((k.a + k.b) * 128) / 34500.0f, 0.7f * ((blocks + 7) / 8)) + k.ends;
+            }
+            if (parts > 1) t += 4.0f + static_cast<float>(parts) * R * M * 8 / 6.0e6f;
+            if (t < least) {
+                least = t;
+                best = {k.kernel, parts};
+            }
+        }
+    }
+    return best;
+}
+
+template <int ASC, int BX, bool WIDE>
+static hipError_t launch(ProductArgs p, int out, float *ws, hipStream_t s) {
+    const ProductPlan plan = product_plan(p.M, p.R, p.Kp, WIDE, ws != nullptr);
+    if constexpr (ASC == 0 && BX == 0) {
+        if (plan.parts > 1) {
+            p.part = ws;
+            variant<ASC, BX, WIDE, 1>(p, plan, s);
+            const unsigned blocks = static_cast<unsigned>((static_cast<size_t>(p.R) * p.M / 4 + 255) / 256);
+            hipLaunchKernelGGL((product_join<WIDE ? 1 : 0>), dim3(blocks), dim3(256), 0, s, p, plan.parts);
+            return hipGetLastError();
+        }
+    }
+    if constexpr (!WIDE) {
+        variant<ASC, BX, WIDE, 0>(p, plan, s);
+    } else if constexpr (ASC == 1) {
+        if (out == 2) variant<ASC, BX, WIDE, 2>(p, plan, s);
+        else variant<ASC, BX, WIDE, 1>(p, plan, s);
+    } else {
+        variant<ASC, BX, WIDE, 1>(p, plan, s);
     }
     return hipGetLastError();
 }
 
-hipError_t launch_product(const ProductArgs &p, bool a_e8m0, int bx, int out, hipStream_t s) {
-    if (a_e8m0) {
-        if (out == 0) return direct<1, 0, 0>(p, s);
-        if (out == 1) return direct<1, 0, 1>(p, s);
-        return direct<1, 0, 2>(p, s);
-    }
-    if (bx == 0) return out == 0 ? direct<0, 0, 0>(p, s) : direct<0, 0, 1>(p, s);
-    if (bx == 1) return out == 0 ? direct<0, 1, 0>(p, s) : direct<0, 1, 1>(p, s);
-    return out == 0 ? direct<0, 2, 0>(p, s) : direct<0, 2, 1>(p, s);
+hipError_t launch_product(const ProductArgs &p, bool a_e8m0, int bx, int out, float *ws, hipStream_t s) {
+    if (a_e8m0) return out == 0 ? launch<1, 0, false>(p, out, ws, s) : launch<1, 0, true>(p, out, ws, s);
+    if (bx == 0) return out == 0 ? launch<0, 0, false>(p, out, ws, s) : launch<0, 0, true>(p, out, ws, s);
+    if (bx == 1) return out == 0 ? launch<0, 1, false>(p, out, ws, s) : launch<0, 1, true>(p, out, ws, s);
+    return out == 0 ? launch<0, 2, false>(p, out, ws, s) : launch<0, 2, true>(p, out, ws, s);
 }
 
 }  // namespace ftmoe

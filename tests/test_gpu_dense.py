@@ -176,6 +176,21 @@ def test_linear(T, N, K):
             assert torch.equal(y, run_linear(N, K, T, wt, x, xd, yd))   # a fixed order of sums
 
 
+@pytest.mark.parametrize("T,N,K", ((700, 1040, 1152), (260, 4096, 2176), (1000, 144, 4096), (3000, 4000, 272), (4097, 4112, 400)))
+def test_linear_many_rows(T, N, K):
+    """The tiled kernels, with and without a split reduction, at rows and features that end inside a tile."""
+    r = rng(T, N, K)
+    wt, w = weight(r, N, K)
+    xv, x = matrix(r, T, K, BF16, spread=1)
+    form, q = form_of(xv)
+    want, mag = q @ w.T, np.abs(q) @ np.abs(w).T
+    for yd in (BF16, F32):
+        assert_product(run_linear(N, K, T, wt, x, BF16, yd), want, mag, K, yd)
+        y = torch.full((T, N), 7.0, dtype=TORCH[yd], device="cuda")
+        ftm.ft_linear({"out_features": N, "in_features": K, "x_dtype": ACT, "y_dtype": yd}, wt, form, T, y)   # no workspace
+        assert_product(y, want, mag, K, yd)
+
+
 def test_linear_long_reduction():
     """K over 512 blocks, one and many rows."""
     r = rng(5)
@@ -243,6 +258,18 @@ def test_weight_grad(T, N, K):
     dw2 = base.clone()
     ftm.ft_linear_weight_grad(N, K, T, dc, xc, dw2, accumulate=True)
     assert_product(dw2, want + f64(base), mag + np.abs(f64(base)), T + 1, F32)
+
+
+@pytest.mark.parametrize("T,N,K", ((900, 1040, 528), (200, 4112, 4000), (5000, 272, 144)))
+def test_weight_grad_of_large_weights_and_long_batches(T, N, K):
+    r = rng(T, N, K, 10)
+    dyv, xv = matrix(r, T, N, BF16, spread=1)[0], matrix(r, T, K, BF16, spread=1)[0]
+    (dc, a), (xc, b) = form_of(dyv.T), form_of(xv.T)
+    want, mag = a @ b.T, np.abs(a) @ np.abs(b).T
+    for dt in (BF16, F32):
+        dw = torch.full((N, K), 3.0, dtype=TORCH[dt], device="cuda")
+        ftm.ft_linear_weight_grad(N, K, T, dc, xc, dw)
+        assert_product(dw, want, mag, T, dt)
 
 
 def test_weight_grad_without_tokens():
