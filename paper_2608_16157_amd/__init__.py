@@ -712,28 +712,40 @@ class ActCodes:
     def c(self) -> ft_act_codes_t:
         return ft_act_codes_t(_ptr(self.codes), _ptr(self.scales))
 
+    def get_device(self) -> int:
+        if self.codes.get_device() != self.scales.get_device():
+            raise ValueError("codes and scales on two devices")
+        return self.codes.get_device()
 
-def _device_of(*tensors) -> torch.device:
-    """The one device of the call's tensors."""
-    dev = None
+
+def _device_of(*tensors) -> int:
+    """Index of the one device that holds the call's tensors."""
+    dev = -1
     for t in tensors:
         if t is None:
             continue
-        for u in ((t.codes, t.scales) if isinstance(t, ActCodes) else (t,)):
-            if dev is None:
-                dev = u.device
-            elif u.device != dev:
-                raise ValueError(f"tensors on {dev} and {u.device}; a call works on one device")
+        d = t.get_device()
+        if d != dev:
+            if dev >= 0:
+                raise ValueError(f"tensors on devices {dev} and {d}; a call works on one device")
+            dev = d
     return dev
 
 
-def _on(device: torch.device, call, *args) -> int:
+# a torch.cuda.Stream object costs a call more than its kernel's launch does
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _on(device: int, call, *args) -> int:
     """``call(*args, stream)`` with ``device`` current; the last of ``args`` is the caller's stream or
     None for that device's current one."""
-    if device.index == torch.cuda.current_device():
-        return call(*args[:-1], _stream(args[-1]))
+    stream = args[-1]
+    stream = _raw_stream(device) if stream is None else _stream(stream)
+    if device == torch.cuda.current_device():
+        return call(*args[:-1], stream)
     with torch.cuda.device(device):
-        return call(*args[:-1], _stream(args[-1]))
+        return call(*args[:-1], stream)
 
 
 def _need_codes(c, name: str, rows: int, cols: int) -> None:

@@ -533,7 +533,8 @@ ProductPlan product_plan(int M, int R, int Kp, bool wide, bool may_split) {
 
 template <int ASC, int BX, bool WIDE>
 static hipError_t launch(ProductArgs p, int out, float *ws, hipStream_t s) {
-    const ProductPlan plan = product_plan(p.M, p.R, p.Kp, WIDE, ws != nullptr);
+    ProductPlan plan{ProductPlan::kDirect16, 1};   // the one that quantises on the way
+    if (BX == 0) plan = product_plan(p.M, p.R, p.Kp, WIDE, ws != nullptr);
     if constexpr (ASC == 0 && BX == 0) {
         if (plan.parts > 1) {
             p.part = ws;
