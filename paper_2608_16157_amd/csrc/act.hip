@@ -23,6 +23,17 @@ struct ActTileShared {
     uint8_t colscale[128];
 };
 
+// One block of a row by one lane row of 16 lanes, 8 values a lane; rows past T (zeros, up to f.Rp) leave only
+// their scale byte.
+__device__ __forceinline__ void put_row(const float (&v)[8], const ActForm &f, long row, int T, int kb, int sub) {
+    const int byte = act_scale_byte(block_mag16(v));
+    const float sc = act_scale_operand(byte);
+    if (row < T)
+        *reinterpret_cast<uint2 *>(f.codes + static_cast<size_t>(row) * f.Kp + kb * 128 + 8 * sub) =
+            uint2{act_codes4(v[0], v[1], v[2], v[3], sc), act_codes4(v[4], v[5], v[6], v[7], sc)};
+    if (sub == 0) f.scales[static_cast<size_t>(kb) * f.Rp + row] = static_cast<uint8_t>(byte);
+}
+
 // Row form of a tile: v holds rows 4 g .. 4 g + 3 (g = the thread's lane row), columns 8 sub .. + 7.
 __device__ __forceinline__ void tile_rows(const float (&v)[kActRows][8], ActTileShared &sh, const ActForm &f, int row0,
                                           int kb, int g, int sub) {
@@ -105,7 +116,26 @@ __global__ __launch_bounds__(kActThreads) void act_quantize(const XT *x, int T, 
     if (col.codes) tile_cols(v, sh, col, cb * 128, rb, g, sub);
 }
 
+// The row form alone: no tile to share, one lane row per (matrix row, block).
+template <class XT>
+__global__ __launch_bounds__(256) void act_quantize_rows(const XT *x, int T, int C, ActForm f) {
+    const int sub = threadIdx.x % 16, kb = blockIdx.y, c = kb * 128 + 8 * sub;
+    const long row = static_cast<long>(blockIdx.x) * 16 + threadIdx.x / 16;   // up to f.Rp
+    float v[8];
+    if (row < T && c < C) load8(x + static_cast<size_t>(row) * C + c, v);
+    else
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = 0.0f;
+    put_row(v, f, row, T, kb, sub);
+}
+
 hipError_t launch_act_quantize(const void *x, bool f32, int T, int C, const ActForm &row, const ActForm &col, hipStream_t s) {
+    if (!col.codes) {
+        const dim3 rows(row.Rp / 16, (C + 127) / 128);
+        if (f32) hipLaunchKernelGGL(act_quantize_rows<float>, rows, dim3(256), 0, s, static_cast<const float *>(x), T, C, row);
+        else hipLaunchKernelGGL(act_quantize_rows<uint16_t>, rows, dim3(256), 0, s, static_cast<const uint16_t *>(x), T, C, row);
+        return hipGetLastError();
+    }
     const dim3 grid((C + 127) / 128, (T + 127) / 128);
     if (f32)
         hipLaunchKernelGGL(act_quantize<float>, grid, dim3(kActThreads), 0, s, static_cast<const float *>(x), T, C, row, col);
@@ -132,18 +162,10 @@ __global__ __launch_bounds__(256) void swiglu_quantize(const XT *gu, int T, int 
     }
 #pragma unroll
     for (int q = 0; q < 8; ++q) hv[q] = silu_f32(g[q]) * u[q];
-    auto put = [&](const float (&v)[8], const ActForm &f, int b) {
-        const int byte = act_scale_byte(block_mag16(v));
-        const float sc = act_scale_operand(byte);
-        if (row < T)
-            *reinterpret_cast<uint2 *>(f.codes + static_cast<size_t>(row) * f.Kp + b * 128 + 8 * sub) =
-                uint2{act_codes4(v[0], v[1], v[2], v[3], sc), act_codes4(v[4], v[5], v[6], v[7], sc)};
-        if (sub == 0) f.scales[static_cast<size_t>(b) * f.Rp + row] = static_cast<uint8_t>(byte);
-    };
-    put(hv, h, kb);
+    put_row(hv, h, row, T, kb, sub);
     if (saved.codes) {
-        put(g, saved, kb);
-        put(u, saved, nkb + kb);
+        put_row(g, saved, row, T, kb, sub);
+        put_row(u, saved, row, T, nkb + kb, sub);
     }
 }
 

@@ -154,7 +154,7 @@ ft_status_t ft_linear(const ft_linear_desc_t *desc, const uint8_t *w, const floa
     if (packed) {
         p.b = static_cast<const uint8_t *>(x);
         p.bs = x_scales;
-    } else if (T <= kDirectTokens) {
+    } else if (T <= kDirectTokens && T * p.Kp <= kDirectBytes) {
         p.x = x;
         bx = desc->x_dtype == FT_DT_BF16 ? 1 : 2;
     } else {

@@ -63,13 +63,17 @@ __global__ __launch_bounds__(256) void product_join(ProductArgs p, int parts) {
 // Direct kernel: operands from global memory to registers, the reduction split over the waves of a
 // workgroup and joined in LDS in a fixed order.  A wave holds 16 RA rows of A and 16 TB rows of B; lane
 // (r = lane % 16, g = lane / 16) the 32 codes [32 g, 32 g + 32) of row r of a block.
-// BX: 0 B is codes; 1 B is bf16, 2 float32, quantised on the way.  ASC: 0 float32 block scales, 1 e8m0.
+// BX: 0 B is codes; 1 B is bf16, 2 float32: then every workgroup first brings the few rows into 8 bits in LDS
+// (the same in all of them: cheaper than a launch for up to kDirectTokens rows).  ASC: 0 float32 block scales, 1 e8m0.
 // WIDE: the arithmetic of float32 results.  OUT: see store4.
 template <int RA, int TB, int W, int ASC, int BX, bool WIDE, int OUT>
 __global__ __launch_bounds__(64 * W) void product_direct(ProductArgs p) {
     constexpr bool kWide = WIDE;
     constexpr int kTile = RA * TB * 256;
+    static_assert(BX == 0 || TB == 1, "quantised rows fit one operand");
     __shared__ float red[W / 2][kTile];
+    __shared__ __attribute__((aligned(16))) uint8_t s_codes[BX ? kDirectBytes : 16];
+    __shared__ uint8_t s_scales[BX ? kDirectBytes / 128 : 1];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = lane_id();
     const int r = lane & 15, g = lane >> 4;
     const int a0 = blockIdx.x * 16 * RA, b0 = blockIdx.y * 16 * TB;
@@ -85,6 +89,25 @@ __global__ __launch_bounds__(64 * W) void product_direct(ProductArgs p) {
     int brow[TB];
 #pragma unroll
     for (int j = 0; j < TB; ++j) brow[j] = min(b0 + 16 * j + r, p.R - 1);
+    if constexpr (BX != 0) {
+        // one lane row of 16 lanes per row and block, 8 values a lane
+        using XT = std::conditional_t<BX == 1, uint16_t, float>;
+        const int sub = threadIdx.x % 16;
+        for (int i = threadIdx.x / 16; i < p.R * nkb; i += 4 * W) {
+            const int row = i / nkb, k = (i - row * nkb) * 128 + 8 * sub;
+            float v[8];
+            if (k < p.K) load8(static_cast<const XT *>(p.x) + static_cast<size_t>(row) * p.K + k, v);   // K is a multiple of 16
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+            const int byte = act_scale_byte(block_mag16(v));
+            const float sc = act_scale_operand(byte);
+            *reinterpret_cast<uint2 *>(s_codes + i * 128 + 8 * sub) =
+                uint2{act_codes4(v[0], v[1], v[2], v[3], sc), act_codes4(v[4], v[5], v[6], v[7], sc)};
+            if (sub == 0) s_scales[i] = static_cast<uint8_t>(byte);
+        }
+        __syncthreads();
+    }
 
     int kb0, kb1;
     split_range(p, nkb, kb0, kb1);
@@ -99,26 +122,8 @@ __global__ __launch_bounds__(64 * W) void product_direct(ProductArgs p) {
                 b[j] = codes32(p.b + static_cast<size_t>(brow[j]) * p.Kp + static_cast<size_t>(kb) * 128 + 16 * g);
                 sb[j] = p.bs[static_cast<size_t>(kb) * p.bsr + brow[j]];
             } else {
-                using XT = std::conditional_t<BX == 1, uint16_t, float>;
-                const XT *x = static_cast<const XT *>(p.x) + static_cast<size_t>(brow[j]) * p.K;
-                float v[32];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int k = kb * 128 + q / 2 * 64 + 16 * g + q % 2 * 8;
-                    if (k < p.K) load8(x + k, v + 8 * q);   // K is a multiple of 16
-                    else
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[8 * q + e] = 0.0f;
-                }
-                uint32_t m = 0;
-#pragma unroll
-                for (int e = 0; e < 32; ++e) m = max(m, act_mag_bits(v[e]));
-                m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16)));
-                m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 32)));
-                sb[j] = act_scale_byte(m);
-                const float sc = act_scale_operand(sb[j]);
-#pragma unroll
-                for (int q = 0; q < 8; ++q) b[j][q] = static_cast<int>(act_codes4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3], sc));
+                b[j] = codes32(s_codes + (brow[j] * nkb + kb) * 128 + 16 * g);
+                sb[j] = s_scales[brow[j] * nkb + kb];
             }
         }
 #pragma unroll
