@@ -68,14 +68,13 @@ ft_status_t balance_status(const ft_balance_desc_t *d) {
 int max_parts(int T) { return std::min(kBalMaxParts, (T + kBalMinPart - 1) / kBalMinPart); }
 
 struct BalanceWs {
-    size_t prob, count, tokens, total;
+    size_t sums, tokens, total;
 };
 BalanceWs balance_ws(const ft_balance_desc_t *d, int T) {
     const size_t rows = static_cast<size_t>(max_parts(std::max(T, 1))) + d->n_seq;
     BalanceWs w;
-    w.prob = 0;
-    w.count = round256(rows * d->n_experts * 4);
-    w.tokens = 2 * w.count;
+    w.sums = 0;
+    w.tokens = round256(rows * d->n_experts * 8);
     w.total = w.tokens + round256(rows * 4);
     return w;
 }
@@ -260,8 +259,7 @@ ft_status_t ft_balance_loss(const ft_balance_desc_t *desc, const float *logits, 
         uint8_t *b = static_cast<uint8_t *>(ws);
         a.part_tokens = (T + max_parts(T) - 1) / max_parts(T);
         a.parts = (T + a.part_tokens - 1) / a.part_tokens;
-        a.ws_prob = reinterpret_cast<float *>(b + w.prob);
-        a.ws_count = reinterpret_cast<int32_t *>(b + w.count);
+        a.ws_sums = reinterpret_cast<float2 *>(b + w.sums);
         a.ws_tokens = reinterpret_cast<int32_t *>(b + w.tokens);
     }
     return launch_balance(a, static_cast<hipStream_t>(stream)) == hipSuccess ? FT_OK : FT_ERR_HIP;

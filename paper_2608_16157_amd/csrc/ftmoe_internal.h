@@ -73,8 +73,7 @@ struct BalanceArgs {
     float *prob, *frac;        // [n_seq][E]
     float *loss;               // [n_seq]
     int parts, part_tokens;    // two-launch form: parts of part_tokens tokens
-    float *ws_prob;            // [parts + n_seq][E]
-    int32_t *ws_count;         // [parts + n_seq][E]
+    float2 *ws_sums;           // [parts + n_seq][E] probability sums, and counts (their bits)
     int32_t *ws_tokens;        // [parts + n_seq]
     // backward
     const float *topk_w, *d_topk_w;   // [T][k] or null
