@@ -16,122 +16,168 @@ constexpr int kActThreads = 512;   // a tile: 32 lane rows of 16 lanes, 4 matrix
 constexpr int kActRows = 4;
 constexpr int kTPad = 132;         // bytes of a transposed row of the tile in LDS
 
+// LDS of a tile of NP planes (matrices of the same shape that leave together).
+template <int NP>
 struct ActTileShared {
-    uint32_t colmax[kActThreads / 16][128];
-    uint8_t t[128 * kTPad];
-    uint8_t rowscale[128];
-    uint8_t colscale[128];
+    uint32_t colmax[NP][kActThreads / 16][64];   // 16 bits a column
+    uint8_t t[NP][128 * kTPad];
+    uint8_t rowscale[NP][128];
+    uint8_t colscale[NP][128];
 };
 
-// One block of a row by one lane row of 16 lanes, 8 values a lane; rows past T (zeros, up to f.Rp) leave only
-// their scale byte.
-__device__ __forceinline__ void put_row(const float (&v)[8], const ActForm &f, long row, int T, int kb, int sub) {
-    const int byte = act_scale_byte(block_mag16(v));
+// Where a plane goes: its row form's block, and the first row of its column form; codes null where not at all.
+struct ActPlane {
+    ActForm row;
+    int row_kb;
+    ActForm col;
+    int col_row0;
+};
+
+// One block of a row by 8 lanes, 16 values a lane; rows past T (zeros, up to f.Rp) leave only their scale byte.
+__device__ __forceinline__ void put_row(const float (&v)[16], const ActForm &f, long row, int T, int kb, int sub) {
+    const int byte = act_scale_byte(block_mag8(v));
     const float sc = act_scale_operand(byte);
     if (row < T)
-        *reinterpret_cast<uint2 *>(f.codes + static_cast<size_t>(row) * f.Kp + kb * 128 + 8 * sub) =
-            uint2{act_codes4(v[0], v[1], v[2], v[3], sc), act_codes4(v[4], v[5], v[6], v[7], sc)};
+        *reinterpret_cast<uint4 *>(f.codes + static_cast<size_t>(row) * f.Kp + kb * 128 + 16 * sub) =
+            uint4{act_codes4(v[0], v[1], v[2], v[3], sc), act_codes4(v[4], v[5], v[6], v[7], sc),
+                  act_codes4(v[8], v[9], v[10], v[11], sc), act_codes4(v[12], v[13], v[14], v[15], sc)};
     if (sub == 0) f.scales[static_cast<size_t>(kb) * f.Rp + row] = static_cast<uint8_t>(byte);
 }
-
-// Row form of a tile: v holds rows 4 g .. 4 g + 3 (g = the thread's lane row), columns 8 sub .. + 7.
-__device__ __forceinline__ void tile_rows(const float (&v)[kActRows][8], ActTileShared &sh, const ActForm &f, int row0,
-                                          int kb, int g, int sub) {
+template <class XT>
+__device__ __forceinline__ void load16(const XT *p, bool in, float (&v)[16]) {
+    if (in) {
+        load8(p, v);
+        load8(p + 8, v + 8);
+    } else {
 #pragma unroll
-    for (int r = 0; r < kActRows; ++r) {
-        const int byte = act_scale_byte(block_mag16(v[r]));
-        const float sc = act_scale_operand(byte);
-        const int row = row0 + kActRows * g + r;
-        if (row < f.R) {
-            const uint2 w = {act_codes4(v[r][0], v[r][1], v[r][2], v[r][3], sc),
-                             act_codes4(v[r][4], v[r][5], v[r][6], v[r][7], sc)};
-            *reinterpret_cast<uint2 *>(f.codes + static_cast<size_t>(row) * f.Kp + kb * 128 + 8 * sub) = w;
-        }
-        if (sub == 0) sh.rowscale[kActRows * g + r] = static_cast<uint8_t>(byte);
+        for (int q = 0; q < 16; ++q) v[q] = 0.0f;
     }
-    __syncthreads();
-    // rows past the last one are zeros here: their scale byte is 127
-    if (threadIdx.x < 8)
-        reinterpret_cast<uint4 *>(f.scales + static_cast<size_t>(kb) * f.Rp + row0)[threadIdx.x] =
-            reinterpret_cast<const uint4 *>(sh.rowscale)[threadIdx.x];
 }
 
-// Column form of a tile: matrix columns become rows col0 .. of f, the tile's 128 matrix rows its block kb.
-__device__ __forceinline__ void tile_cols(const float (&v)[kActRows][8], ActTileShared &sh, const ActForm &f, int col0,
-                                          int kb, int g, int sub) {
-    const int t = threadIdx.x;
+// A tile of 128 x 128 elements: v[n] holds plane n's rows 4 g .. 4 g + 3 (g: the thread's lane row), columns
+// 8 sub .. 8 sub + 7 of it.  Matrix rows row0 .., block col_kb of the column forms.
+//
+// A column's scale depends on its largest magnitude only through the exponent and through whether the mantissa
+// is above 1.75: the upper 16 bits, rounded up, decide it exactly, so two columns share a word of LDS.
+template <int NP>
+__device__ __forceinline__ void put_tile(const float (&v)[NP][kActRows][8], ActTileShared<NP> &sh, const ActPlane (&to)[NP],
+                                         int row0, int col_kb) {
+    const int t = threadIdx.x, g = t / 16, sub = t % 16;
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-        uint32_t m = 0;
+    for (int n = 0; n < NP; ++n) {
+        if (to[n].row.codes) {
+            const ActForm &f = to[n].row;
 #pragma unroll
-        for (int r = 0; r < kActRows; ++r) m = max(m, act_mag_bits(v[r][c]));
-        sh.colmax[g][8 * sub + c] = m;
+            for (int r = 0; r < kActRows; ++r) {
+                const int byte = act_scale_byte(block_mag16(v[n][r])), row = row0 + kActRows * g + r;
+                const float sc = act_scale_operand(byte);
+                if (row < f.R)
+                    *reinterpret_cast<uint2 *>(f.codes + static_cast<size_t>(row) * f.Kp + to[n].row_kb * 128 + 8 * sub) =
+                        uint2{act_codes4(v[n][r][0], v[n][r][1], v[n][r][2], v[n][r][3], sc),
+                              act_codes4(v[n][r][4], v[n][r][5], v[n][r][6], v[n][r][7], sc)};
+                if (sub == 0) sh.rowscale[n][kActRows * g + r] = static_cast<uint8_t>(byte);
+            }
+        }
+        if (to[n].col.codes) {
+            uint32_t m[8];
+            float all = 0.0f;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                const float f = max3_abs(max3_abs(0.0f, v[n][0][c], v[n][1][c]), v[n][2][c], v[n][3][c]);
+                all += f;   // not finite if one of them is not
+                m[c] = __float_as_uint(f) + 0xFFFFu;
+            }
+            if (!(all < INFINITY))   // as in mag_of
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    m[c] = max(max(act_mag_bits(v[n][0][c]), act_mag_bits(v[n][1][c])),
+                               max(act_mag_bits(v[n][2][c]), act_mag_bits(v[n][3][c]))) + 0xFFFFu;
+            *reinterpret_cast<uint4 *>(&sh.colmax[n][g][4 * sub]) =
+                uint4{m[0] >> 16 | (m[1] & 0xFFFF0000u), m[2] >> 16 | (m[3] & 0xFFFF0000u),
+                      m[4] >> 16 | (m[5] & 0xFFFF0000u), m[6] >> 16 | (m[7] & 0xFFFF0000u)};
+        }
     }
     __syncthreads();
-    if (t < 128) {
+    for (int i = t; i < NP * 128; i += kActThreads) {
+        const int n = i / 128, c = i % 128;
         uint32_t m = 0;
 #pragma unroll 8
-        for (int i = 0; i < kActThreads / 16; ++i) m = max(m, sh.colmax[i][t]);
-        sh.colscale[t] = static_cast<uint8_t>(act_scale_byte(m));
+        for (int q = 0; q < kActThreads / 16; ++q) m = max(m, (sh.colmax[n][q][c / 2] >> (16 * (c % 2))) & 0xFFFFu);
+        sh.colscale[n][c] = static_cast<uint8_t>(act_scale_byte(m << 16));
     }
     __syncthreads();
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-        const float sc = act_scale_operand(sh.colscale[8 * sub + c]);
-        *reinterpret_cast<uint32_t *>(sh.t + (8 * sub + c) * kTPad + kActRows * g) =
-            act_codes4(v[0][c], v[1][c], v[2][c], v[3][c], sc);
-    }
+    for (int n = 0; n < NP; ++n)
+        if (to[n].col.codes)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                const float sc = act_scale_operand(sh.colscale[n][8 * sub + c]);
+                *reinterpret_cast<uint32_t *>(sh.t[n] + (8 * sub + c) * kTPad + kActRows * g) =
+                    act_codes4(v[n][0][c], v[n][1][c], v[n][2][c], v[n][3][c], sc);
+            }
     __syncthreads();
 #pragma unroll
-    for (int i = t; i < 128 * 8; i += kActThreads) {
-        const int c = i / 8, p = i % 8;
-        if (col0 + c < f.R) {
-            const uint32_t *s = reinterpret_cast<const uint32_t *>(sh.t + c * kTPad + 16 * p);
-            *reinterpret_cast<uint4 *>(f.codes + static_cast<size_t>(col0 + c) * f.Kp + kb * 128 + 16 * p) =
-                uint4{s[0], s[1], s[2], s[3]};
+    for (int n = 0; n < NP; ++n) {
+        // rows past the last one are zeros here: their scale byte is 127
+        if (to[n].row.codes && t < 8)
+            reinterpret_cast<uint4 *>(to[n].row.scales + static_cast<size_t>(to[n].row_kb) * to[n].row.Rp + row0)[t] =
+                reinterpret_cast<const uint4 *>(sh.rowscale[n])[t];
+        if (!to[n].col.codes) continue;
+        const ActForm &f = to[n].col;
+#pragma unroll
+        for (int i = t; i < 128 * 8; i += kActThreads) {
+            const int c = i / 8, p = i % 8;
+            if (to[n].col_row0 + c < f.R) {
+                const uint32_t *s = reinterpret_cast<const uint32_t *>(sh.t[n] + c * kTPad + 16 * p);
+                *reinterpret_cast<uint4 *>(f.codes + static_cast<size_t>(to[n].col_row0 + c) * f.Kp + col_kb * 128 + 16 * p) =
+                    uint4{s[0], s[1], s[2], s[3]};
+            }
         }
+        if (t >= 64 && t < 72)
+            reinterpret_cast<uint4 *>(f.scales + static_cast<size_t>(col_kb) * f.Rp + to[n].col_row0)[t - 64] =
+                reinterpret_cast<const uint4 *>(sh.colscale[n])[t - 64];
     }
-    if (t < 8)
-        reinterpret_cast<uint4 *>(f.scales + static_cast<size_t>(kb) * f.Rp + col0)[t] =
-            reinterpret_cast<const uint4 *>(sh.colscale)[t];
-    __syncthreads();   // the tile's LDS may be written again
 }
 
-// One 128 x 128 tile of x [T][C] per workgroup; row.codes or col.codes may be null.
+// One 128 x 128 tile of x [T][C] per workgroup; row.codes may be null.
 template <class XT>
 __global__ __launch_bounds__(kActThreads) void act_quantize(const XT *x, int T, int C, ActForm row, ActForm col) {
-    __shared__ __attribute__((aligned(16))) ActTileShared sh;
+    __shared__ __attribute__((aligned(16))) ActTileShared<1> sh;
     const int g = threadIdx.x / 16, sub = threadIdx.x % 16;
     const int cb = blockIdx.x, rb = blockIdx.y;
-    float v[kActRows][8];
+    float v[1][kActRows][8];
 #pragma unroll
     for (int r = 0; r < kActRows; ++r) {
         const int i = rb * 128 + kActRows * g + r, c = cb * 128 + 8 * sub;
-        if (i < T && c < C) load8(x + static_cast<size_t>(i) * C + c, v[r]);   // C is a multiple of 16
+        if (i < T && c < C) load8(x + static_cast<size_t>(i) * C + c, v[0][r]);   // C is a multiple of 16
         else
 #pragma unroll
-            for (int q = 0; q < 8; ++q) v[r][q] = 0.0f;
+            for (int q = 0; q < 8; ++q) v[0][r][q] = 0.0f;
     }
-    if (row.codes) tile_rows(v, sh, row, rb * 128, cb, g, sub);
-    if (col.codes) tile_cols(v, sh, col, cb * 128, rb, g, sub);
+    const ActPlane to[1] = {{row, cb, col, cb * 128}};
+    put_tile<1>(v, sh, to, rb * 128, rb);
 }
 
-// The row form alone: no tile to share, one lane row per (matrix row, block).
+// The row form alone: no tile to share, 8 lanes per (matrix row, block), two rows on the way at once.  The blocks
+// of a row are consecutive workgroups, so that what runs together reads whole rows.
+constexpr int kRowsPerLane = 2, kRowsPerWg = 32 * kRowsPerLane;
 template <class XT>
 __global__ __launch_bounds__(256) void act_quantize_rows(const XT *x, int T, int C, ActForm f) {
-    const int sub = threadIdx.x % 16, kb = blockIdx.y, c = kb * 128 + 8 * sub;
-    const long row = static_cast<long>(blockIdx.x) * 16 + threadIdx.x / 16;   // up to f.Rp
-    float v[8];
-    if (row < T && c < C) load8(x + static_cast<size_t>(row) * C + c, v);
-    else
+    const int sub = threadIdx.x % 8, kb = blockIdx.x, c = kb * 128 + 16 * sub;
+    const long row0 = static_cast<long>(blockIdx.y) * kRowsPerWg + threadIdx.x / 8;   // rows up to f.Rp
+    float v[kRowsPerLane][16];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = 0.0f;
-    put_row(v, f, row, T, kb, sub);
+    for (int r = 0; r < kRowsPerLane; ++r) {
+        const long row = row0 + 32 * r;
+        load16(x + static_cast<size_t>(row) * C + c, row < T && c < C, v[r]);   // C is a multiple of 16
+    }
+#pragma unroll
+    for (int r = 0; r < kRowsPerLane; ++r) put_row(v[r], f, row0 + 32 * r, T, kb, sub);
 }
 
 hipError_t launch_act_quantize(const void *x, bool f32, int T, int C, const ActForm &row, const ActForm &col, hipStream_t s) {
     if (!col.codes) {
-        const dim3 rows(row.Rp / 16, (C + 127) / 128);
+        const dim3 rows((C + 127) / 128, row.Rp / kRowsPerWg);
         if (f32) hipLaunchKernelGGL(act_quantize_rows<float>, rows, dim3(256), 0, s, static_cast<const float *>(x), T, C, row);
         else hipLaunchKernelGGL(act_quantize_rows<uint16_t>, rows, dim3(256), 0, s, static_cast<const uint16_t *>(x), T, C, row);
         return hipGetLastError();
@@ -146,22 +192,17 @@ hipError_t launch_act_quantize(const void *x, bool f32, int T, int C, const ActF
 }
 
 // SwiGLU forward: h = silu(g) u from gu [T][2 I] (gate columns first), h in the row form and, if asked for,
-// gu itself.  One lane row per (matrix row, block of 128 channels of h).
+// gu itself.  8 lanes per (matrix row, block of 128 channels of h).
 template <class XT>
 __global__ __launch_bounds__(256) void swiglu_quantize(const XT *gu, int T, int I, ActForm h, ActForm saved) {
-    const int sub = threadIdx.x % 16, kb = blockIdx.y, nkb = I / 128;
-    const long row = static_cast<long>(blockIdx.x) * 16 + threadIdx.x / 16;   // up to h.Rp
-    float g[8], u[8], hv[8];
-    if (row < T) {
-        const XT *p = gu + static_cast<size_t>(row) * 2 * I + kb * 128 + 8 * sub;
-        load8(p, g);
-        load8(p + I, u);
-    } else {
+    const int sub = threadIdx.x % 8, kb = blockIdx.x, nkb = I / 128;
+    const long row = static_cast<long>(blockIdx.y) * 32 + threadIdx.x / 8;   // up to h.Rp
+    const XT *p = gu + static_cast<size_t>(row) * 2 * I + kb * 128 + 16 * sub;
+    float g[16], u[16], hv[16];
+    load16(p, row < T, g);
+    load16(p + I, row < T, u);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) g[q] = u[q] = 0.0f;
-    }
-#pragma unroll
-    for (int q = 0; q < 8; ++q) hv[q] = silu_f32(g[q]) * u[q];
+    for (int q = 0; q < 16; ++q) hv[q] = silu_f32(g[q]) * u[q];
     put_row(hv, h, row, T, kb, sub);
     if (saved.codes) {
         put_row(g, saved, row, T, kb, sub);
@@ -171,7 +212,7 @@ __global__ __launch_bounds__(256) void swiglu_quantize(const XT *gu, int T, int 
 
 hipError_t launch_swiglu_quantize(const void *gu, bool f32, int T, int I, const ActForm &h, const ActForm &saved,
                                   hipStream_t s) {
-    const dim3 grid(h.Rp / 16, I / 128);
+    const dim3 grid(I / 128, h.Rp / 32);
     if (f32)
         hipLaunchKernelGGL(swiglu_quantize<float>, grid, dim3(256), 0, s, static_cast<const float *>(gu), T, I, h, saved);
     else
@@ -180,14 +221,15 @@ hipError_t launch_swiglu_quantize(const void *gu, bool f32, int T, int I, const 
     return hipGetLastError();
 }
 
-// SwiGLU backward.  With s = 1 / (1 + exp(-g)):  h = g s u,  dg = dh u s (1 + g (1 - s)),  du = dh g s.
+// SwiGLU backward.  With s = 1 / (1 + exp(-g)):  h = g s u,  dg = dh u s (1 + g (1 - s)),  du = dh g s.  The
+// reciprocal is the hardware's, 1 ulp; results have 4 significant bits.
 template <class XT>
-__global__ __launch_bounds__(kActThreads) void swiglu_backward(ActForm saved, const XT *dh, int T, int I, ActForm drow,
-                                                               ActForm dcol, ActForm hcol) {
-    __shared__ __attribute__((aligned(16))) ActTileShared sh;
+__global__ __launch_bounds__(kActThreads, 4) void swiglu_backward(ActForm saved, const XT *dh, int T, int I, ActForm drow,
+                                                                  ActForm dcol, ActForm hcol) {
+    __shared__ __attribute__((aligned(16))) ActTileShared<3> sh;
     const int lr = threadIdx.x / 16, sub = threadIdx.x % 16;
     const int cb = blockIdx.x, rb = blockIdx.y, nkb = I / 128;
-    float dg[kActRows][8], du[kActRows][8], h[kActRows][8];
+    float v[3][kActRows][8];   // dg, du, h
 #pragma unroll
     for (int r = 0; r < kActRows; ++r) {
         const int i = rb * 128 + kActRows * lr + r;
@@ -204,29 +246,19 @@ __global__ __launch_bounds__(kActThreads) void swiglu_backward(ActForm saved, co
             load8(dh + static_cast<size_t>(i) * I + cb * 128 + 8 * sub, d);
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
-                const float e = __expf(-g[q]), s = 1.0f / (1.0f + e);
+                const float s = __builtin_amdgcn_rcpf(1.0f + __expf(-g[q]));   // 0 where exp overflows
                 const float gs = g[q] * s;
-                h[r][q] = gs * u[q];
-                du[r][q] = d[q] * gs;
-                // 1 - s = e s; where e overflows s is 0 and 1 - s is 1
-                const float one_s = s > 0.0f ? e * s : 1.0f;
-                dg[r][q] = d[q] * u[q] * (s + gs * one_s);
+                v[2][r][q] = gs * u[q];
+                v[1][r][q] = d[q] * gs;
+                v[0][r][q] = d[q] * u[q] * (s + gs * (1.0f - s));
             }
         } else {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) h[r][q] = du[r][q] = dg[r][q] = 0.0f;
+            for (int q = 0; q < 8; ++q) v[0][r][q] = v[1][r][q] = v[2][r][q] = 0.0f;
         }
     }
-    if (drow.codes) {
-        tile_rows(dg, sh, drow, rb * 128, cb, lr, sub);
-        __syncthreads();
-        tile_rows(du, sh, drow, rb * 128, nkb + cb, lr, sub);
-    }
-    if (dcol.codes) {
-        tile_cols(dg, sh, dcol, cb * 128, rb, lr, sub);
-        tile_cols(du, sh, dcol, I + cb * 128, rb, lr, sub);
-    }
-    if (hcol.codes) tile_cols(h, sh, hcol, cb * 128, rb, lr, sub);
+    const ActPlane to[3] = {{drow, cb, dcol, cb * 128}, {drow, nkb + cb, dcol, I + cb * 128}, {ActForm{}, 0, hcol, cb * 128}};
+    put_tile<3>(v, sh, to, rb * 128, rb);
 }
 
 hipError_t launch_swiglu_backward(const ActForm &saved, const void *dh, bool f32, int T, int I, const ActForm &drow,

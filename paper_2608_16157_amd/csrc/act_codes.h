@@ -83,12 +83,37 @@ __device__ __forceinline__ void load8(const float *p, float *v) {
     }
 }
 
-// largest magnitude of 8 values over the 16 lanes of this lane's row (128 values), in every lane of it
-__device__ __forceinline__ uint32_t block_mag16(const float *v) {
-    uint32_t m = 0;
+// max(m, |a|, |b|) in one instruction.  The compiler takes four: it clears the signs and quiets the operands
+// first.  NaN operands drop out or make the result NaN; both are looked after where it is used.
+__device__ __forceinline__ float max3_abs(float m, float a, float b) {
+    float r;
+    asm("v_max3_f32 %0, %1, |%2|, |%3|" : "=v"(r) : "v"(m), "v"(a), "v"(b));
+    return r;
+}
+
+// Largest finite magnitude of N values (N even).  The plain maximum first: only what is not finite reaches the
+// bits of infinity, and then the values are looked at again one by one.
+template <int N>
+__device__ __forceinline__ uint32_t mag_of(const float *v) {
+    float f = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, act_mag_bits(v[i]));
-    return row_max_u32(m);
+    for (int i = 0; i < N; i += 2) f = max3_abs(f, v[i], v[i + 1]);
+    uint32_t m = __float_as_uint(f);
+    if (m >= 0x7F800000u) {
+        m = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) m = max(m, act_mag_bits(v[i]));
+    }
+    return m;
+}
+
+// a block's 128 values: 8 in each of the 16 lanes of a lane row, or 16 in each of the 8 lanes of half of one
+__device__ __forceinline__ uint32_t block_mag16(const float *v) { return row_max_u32(mag_of<8>(v)); }
+__device__ __forceinline__ uint32_t block_mag8(const float *v) {
+    uint32_t m = mag_of<16>(v);
+    m = max(m, dpp_u32<0xB1>(m));       // quad_perm: lane ^ 1
+    m = max(m, dpp_u32<0x4E>(m));       // quad_perm: lane ^ 2
+    return max(m, dpp_u32<0x141>(m));   // row_half_mirror: 7 - lane
 }
 
 // float32 -> bf16, round to nearest even; NaN stays NaN

@@ -138,8 +138,14 @@ def test_quantize_of_extreme_values():
     x[6, :4] = (np.inf, -np.inf, np.nan, 7.0)
     x[7, 200] = -np.inf
     x[8] = 2.0 ** np.linspace(-149, 0, 256)
+    # a signalling NaN in an otherwise ordinary block
+    x.view(np.uint32)[2, 130] = 0x7F800001
+    x.view(np.uint32)[3, 131] = 0xFF810000
     row, col = filled(9, 256), filled(256, 9)
     ftm.ft_act_quantize(cuda(x), 9, 256, row, col)
+    alone = filled(9, 256)
+    ftm.ft_act_quantize(cuda(x), 9, 256, row=alone)
+    assert torch.equal(alone.codes, row.codes) and torch.equal(alone.scales, row.scales)
     for c, v in ((row, x), (col, x.T)):
         codes, s = dense.quantize(v.astype(np.float64))
         got = c.codes.cpu().numpy()
