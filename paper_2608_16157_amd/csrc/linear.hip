@@ -316,24 +316,40 @@ __global__ __launch_bounds__(64 * GA * GB, 2) void product_tiled(ProductArgs p, 
         static_for<0, WA>([&](auto ii) {
             constexpr int I = decltype(ii)::value, P = (I + WA - 1) % WA, N = (I + 1) % WA;
             constexpr bool kMid = I == HS - 1, kLast = I == WA - 1;
-            if constexpr (kMid || kLast) {
+            constexpr bool kHandOff = kMid || kLast;
+            i32x8_vec_t an;
+            int san = 127;
+            auto hand_off = [&] {
                 wait_vmcnt<kInFlight>();
                 wait_lgkmcnt0();
                 stage_barrier();
-            }
-            // requests number Q of the step's WB groups
-            auto requests = [&](auto qq) {
-                constexpr int Q = decltype(qq)::value;
-                if constexpr (kMid) {
-                    static_for<Q * (BI + 1) / WB, (Q + 1) * (BI + 1) / WB>([&](auto i) { request_b(i, kb + 2); });
-                    if constexpr (Q == WB - 1) all_a(ic<1>{}, kb + 2, s0);
-                }
-                if constexpr (kLast && Q == 0) all_a(ic<0>{}, kb + 3, s1);
             };
-            if constexpr (kWide) static_for<0, WB>(requests);
-            const i32x8_vec_t an = operand(la + (kLast ? s2 : N < HS ? s0 : s1) + N % HS * 2048);
-            if constexpr (kLast) sw_next = weight_scale(sn);
-            const int san = ASC ? las[kLast ? sn : (kb & 3) * 512 + N * 16] : 127;
+            auto read_next = [&] {
+                an = operand(la + (kLast ? s2 : N < HS ? s0 : s1) + N % HS * 2048);
+                if constexpr (kLast) sw_next = weight_scale(sn);
+                if (ASC) san = las[kLast ? sn : (kb & 3) * 512 + N * 16];
+            };
+            // the requests into the places that a hand-off freed, spread over the steps up to the next one:
+            // behind matrix instruction J of this step
+            auto requests = [&](auto jj) {
+                constexpr int J = decltype(jj)::value, M = BI + 1 + AH;
+                static_for<0, M>([&](auto i) {
+                    constexpr int Q = decltype(i)::value;
+                    if constexpr (Q * HS * WB / M == (I - (HS - 1)) * WB + J) {
+                        if constexpr (Q <= BI) request_b(i, kb + 2);
+                        else request_a(ic<1>{}, ic<Q - BI - 1>{}, kb + 2, s0);
+                    }
+                });
+                if constexpr (kLast)
+                    static_for<0, AH>([&](auto i) {
+                        if constexpr (decltype(i)::value * WB / AH == J) request_a(ic<0>{}, i, kb + 3, s1);
+                    });
+            };
+            if constexpr (kWide) {
+                if constexpr (kHandOff) hand_off();
+                static_for<0, WB>(requests);
+            }
+            if constexpr (kWide || !kHandOff) read_next();
             if constexpr (kWide) {
                 floatx4_t zn[WB];
 #pragma unroll
@@ -363,7 +379,8 @@ __global__ __launch_bounds__(64 * GA * GB, 2) void product_tiled(ProductArgs p, 
                 }
             } else {
                 // in program order: one matrix instruction, the scale of the sums kLag instructions back, and
-                // in the last step the next block's operand into the registers the instruction has just read
+                // in the last step the next block's operand into the registers the instruction has just
+                // read.  A hand-off comes behind the step's first instruction, which covers it.
                 __builtin_amdgcn_sched_barrier(0);
                 static_for<0, WB>([&](auto jj) {
                     constexpr int J = decltype(jj)::value;
@@ -376,6 +393,11 @@ __global__ __launch_bounds__(64 * GA * GB, 2) void product_tiled(ProductArgs p, 
                         for (int q = 0; q < 4; ++q)
                             acc[F / WB][F % WB][q] = fmaf(f, z[F % kLag][q], acc[F / WB][F % WB][q]);
                         z[T % kLag] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b[J], floatx4_t{}, 0, 0, 0, sa, 0, sb[J]);
+                    }
+                    if constexpr (kHandOff && J == 0) {
+                        __builtin_amdgcn_sched_barrier(0);
+                        hand_off();
+                        read_next();
                     }
                     requests(jj);
                     if constexpr (kLast) {
