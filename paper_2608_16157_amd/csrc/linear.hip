@@ -248,7 +248,7 @@ __global__ __launch_bounds__(64 * GA * GB, 2) void product_tiled(ProductArgs p, 
                           : ASC    ? min(a0 + 4 * lane, p.asr - 4)
                                    : static_cast<uint32_t>(min(a0 / 128 + lane / 32, (p.M - 1) / 128)) * (p.Kp / 128) * 4;
     const uint32_t l0 = lds_address(lds);
-    // past the last block the requests repeat it
+    // the first requests repeat the last block where there are fewer
     auto request_a = [&](auto half, auto i, int kb, int slot) {
         constexpr int H = decltype(half)::value, I = decltype(i)::value;
         dma16(abase + static_cast<size_t>(min(kb, nkb - 1)) * 128, aoff[H][I], l0 + slot + (wave * AH + I) * 1024);
@@ -305,7 +305,9 @@ __global__ __launch_bounds__(64 * GA * GB, 2) void product_tiled(ProductArgs p, 
     float sw = weight_scale(0), swz_old = 0.0f;   // weight scale of this block, and of the sums in z
     int s0 = 0;                                   // A slot of the block's first half
     auto after = [&](int slot) { return slot + kHalf == kAHalves * kHalf ? 0 : slot + kHalf; };
-    for (int kb = 0; kb < nkb; ++kb) {
+    // one block; `more`: there are blocks to request
+    auto block = [&](int kb, auto more) {
+        constexpr bool kMore = decltype(more)::value;
         const int s1 = after(s0), s2 = after(s1), bn = ((kb + 1) & 1) * kBBlock, sn = ((kb + 1) & 3) * 512;
         float sw_next = sw;
         if constexpr (kWide)
@@ -320,7 +322,7 @@ __global__ __launch_bounds__(64 * GA * GB, 2) void product_tiled(ProductArgs p, 
             i32x8_vec_t an;
             int san = 127;
             auto hand_off = [&] {
-                wait_vmcnt<kInFlight>();
+                wait_vmcnt<kMore ? kInFlight : 0>();
                 wait_lgkmcnt0();
                 stage_barrier();
             };
@@ -333,14 +335,14 @@ __global__ __launch_bounds__(64 * GA * GB, 2) void product_tiled(ProductArgs p, 
             // behind matrix instruction J of this step
             auto requests = [&](auto jj) {
                 constexpr int J = decltype(jj)::value, M = BI + 1 + AH;
-                static_for<0, M>([&](auto i) {
+                if constexpr (kMore) static_for<0, M>([&](auto i) {
                     constexpr int Q = decltype(i)::value;
                     if constexpr (Q * HS * WB / M == (I - (HS - 1)) * WB + J) {
                         if constexpr (Q <= BI) request_b(i, kb + 2);
                         else request_a(ic<1>{}, ic<Q - BI - 1>{}, kb + 2, s0);
                     }
                 });
-                if constexpr (kLast)
+                if constexpr (kMore && kLast)
                     static_for<0, AH>([&](auto i) {
                         if constexpr (decltype(i)::value * WB / AH == J) request_a(ic<0>{}, i, kb + 3, s1);
                     });
@@ -413,22 +415,45 @@ __global__ __launch_bounds__(64 * GA * GB, 2) void product_tiled(ProductArgs p, 
         swz_old = sw;
         sw = sw_next;
         s0 = s2;
-    }
-    wait_vmcnt<0>();   // the requests past the end
+    };
+    int kb = 0;
+    for (; kb < nkb - 2; ++kb) block(kb, ic<1>{});
+    for (; kb < nkb; ++kb) block(kb, ic<0>{});
+    wait_vmcnt<0>();
     if constexpr (!ASC)
 #pragma unroll
         for (int j = 0; j < WB; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) acc[WA - 1][j][q] = fmaf(swz_old, z[j][q], acc[WA - 1][j][q]);
+    // Through LDS, 16 rows of B at a time and each wave by itself, so that whole lines leave: as the sums lie in
+    // the registers, a store would write 32 bytes of each of 16 rows (8192 x 4096 results: 28 us for K = 128 against 21).
+    constexpr int kSize = OUT == 0 ? 2 : 4, kRow = 16 * WA * kSize, kPitch = kRow + 16, kLanes = kRow / 16;
+    static_assert(16 * kPitch * NW <= sizeof(lds), "epilogue");
+    stage_barrier();   // every wave has read its last operands, and its requests have landed
+    uint8_t *mine = lds + wave * 16 * kPitch;
 #pragma unroll
     for (int j = 0; j < WB; ++j) {
-        const int bi = b0 + (wb * WB + j) * 16 + r;
-        if (bi >= p.R) continue;
 #pragma unroll
         for (int i = 0; i < WA; ++i) {
-            const int ai = a0 + (wa * WA + i) * 16 + 4 * g;
-            if (ai < p.M) store4<OUT>(split_out(p), static_cast<size_t>(bi) * p.M + ai, acc[i][j]);
+            uint8_t *at = mine + r * kPitch + (16 * i + 4 * g) * kSize;
+            if constexpr (OUT == 0)
+                *reinterpret_cast<uint2 *>(at) = uint2{f32_to_bf16_any(acc[i][j][0]) | f32_to_bf16_any(acc[i][j][1]) << 16,
+                                                       f32_to_bf16_any(acc[i][j][2]) | f32_to_bf16_any(acc[i][j][3]) << 16};
+            else *reinterpret_cast<floatx4_t *>(at) = acc[i][j];
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // a wave's own LDS operations execute in order
+        const int ai = a0 + wa * WA * 16 + lane % kLanes * (16 / kSize);   // M is a multiple of 16
+#pragma unroll
+        for (int q = 0; q < 16; q += 64 / kLanes) {
+            const int row = q + lane / kLanes, bi = b0 + (wb * WB + j) * 16 + row;
+            const u32x4_t v = *reinterpret_cast<const u32x4_t *>(mine + row * kPitch + lane % kLanes * 16);
+            if (bi < p.R && ai < p.M) {
+                u32x4_t *o = reinterpret_cast<u32x4_t *>(static_cast<uint8_t *>(split_out(p)) + (static_cast<size_t>(bi) * p.M + ai) * kSize);
+                if constexpr (OUT == 2) *reinterpret_cast<floatx4_t *>(o) += __builtin_bit_cast(floatx4_t, v);
+                else *o = v;
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 
