@@ -56,7 +56,14 @@ __global__ __launch_bounds__(256) void product_join(ProductArgs p, int parts) {
     const size_t n = static_cast<size_t>(p.R) * p.M, i = (static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
     if (i >= n) return;
     floatx4_t v = *reinterpret_cast<const floatx4_t *>(p.part + i);
-    for (int z = 1; z < parts; ++z) v += *reinterpret_cast<const floatx4_t *>(p.part + z * n + i);
+    for (int z = 1; z < parts; z += 4) {   // four parts on the way at a time; behind the last one it again, unused
+        floatx4_t part[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) part[q] = *reinterpret_cast<const floatx4_t *>(p.part + min(z + q, parts - 1) * n + i);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (z + q < parts) v += part[q];
+    }
     store4<OUT>(p.out, i, v);
 }
 
@@ -190,12 +197,18 @@ __global__ __launch_bounds__(64 * W) void product_direct(ProductArgs p) {
 // walks the A operands, one per step: each step reads the next A operand while the matrix instructions of
 // the current one run, and the float32 scale of the sums before is applied between them.
 //
-// What bounds it is how fast L2 fills LDS, and that is a matter of bytes in flight.  B's place in LDS is
-// free as soon as the block's operands are in registers, A's half by half, so B lies in a ring of two
-// blocks and A in one of five half blocks, and everything is requested about two blocks before it is
-// read.  The two hand-offs of a block, in the last step of each half: wait for what the next step reads
-// (requests return in order, so the younger ones may stay in flight) and for this wave's own LDS reads,
-// barrier, and request into the freed places between the step's matrix instructions.
+// B's place in LDS is free as soon as the block's operands are in registers, A's half by half, so B lies in
+// a ring of two blocks and A in one of five half blocks, and everything is requested about two blocks
+// before it is read.  The two hand-offs of a block, in the last step of each half: wait for what the next
+// step reads (requests return in order, so the younger ones may stay in flight) and for this wave's own
+// LDS reads, barrier, and request into the freed places between the step's matrix instructions.
+//
+// What bounds it, at 8192 x 4096 x 7168 (201 us, 2390 TFLOP/s; the library's largest fp8 product, without
+// block scales, reaches 3110, and 2800 at this size): the matrix units are busy 0.65 of the time inside the
+// loop, at a clock of 1.85 to 2.0 GHz, where power holds it (2.4 when it does not).  What takes the rest, timed by
+// leaving it out: issuing the requests 30 us, the barriers 15, the float32 scale of every sum 20; waiting for
+// data 2 and its way through L2 (81 % hits, two patches of tiles compared) nothing.  32 x 32 instructions,
+// behind which the scale hides whole, draw more power: 206 us at the same busy share and a lower clock.
 template <int WA, int WB, int GA, int GB, int ASC, bool WIDE, int OUT>
 __global__ __launch_bounds__(64 * GA * GB, 2) void product_tiled(ProductArgs p, int na, int nb) {
     constexpr bool kWide = WIDE;
@@ -529,25 +542,27 @@ static void variant(const ProductArgs &p, const ProductPlan &plan, hipStream_t s
 }
 
 // Which kernel runs a product, and into how many parts its reduction is split: the least of their estimated
-// times.  The estimate is a workgroup's blocks times what one takes (in microseconds, measured on this
-// card over N from 512 to 7168, K from 768 to 16384 and 16 to 8192 rows), as often as its workgroups
-// outnumber the 256 CUs, plus each round's start and end, plus the join of the parts:
-//   direct kernels  the bytes of a block at 34.5 GB/s a CU (the waves of a CU share that rate), at least
-//                   0.7 for every 8 blocks: a small reduction is one round trip to memory
-//   64 x 64         0.58 a block alone on its CU, 0.61 shared, whatever the arithmetic
-//   128 x 128       0.55 alone, 0.60 shared by two; widened 1.05 and 0.95
-//   256 x 256       1.63 rising to 1.9 when every CU has one
-// With M = 4096, K = 7168 (estimate / measured): 32 rows 12.9 / 12.7 (2 parts of 32 x 32 tiles), unsplit
-// 13.1 / 12.9 (16 x 32); 256 rows 20 / 20.4 (128 x 128, 4 parts), unsplit 35 / 34; 777 rows 35 / 38,
-// 2 parts 43 / 44; 4096 rows 115 / 110 (256 x 256), 138 / 136 (128 x 128).
+// times.  The estimate is a workgroup's blocks times what one takes (in microseconds, fitted to times on this
+// card over ten weights, N from 512 to 8192, K from 512 to 18432, at 16 to 8192 rows, every kernel and split
+// of each: the rule's choice is 1.0 % above the best of them in the mean, 19 % at the worst), as often as its
+// workgroups outnumber the 256 CUs, plus each round's start and end, plus the join of the parts:
+//   direct kernels  the bytes of a block at 33.4 GB/s a CU (the waves of a CU share that rate), at least
+//                   0.43 for every 8 blocks: a small reduction is one round trip to memory
+//   64 x 64         0.58 a block alone on its CU, 0.53 shared, whatever the arithmetic
+//   128 x 128       0.51 alone, 0.47 shared by two; widened 0.96 and 0.76
+//   256 x 256       1.19 rising to 1.43 when every CU has one
+//   join            2.3 and the parts' bytes, written and read, at 4.65 TB/s
+// With M = 4096, K = 7168 (estimate / measured): 32 rows 13.1 / 13.1 (16 x 32 tiles), as 8 parts of 128 x 128
+// 12.5 / 13.0; 256 rows 21.5 / 19.8 (128 x 128, 4 parts), 2 parts 25 / 23.7; 777 rows 33 / 36,
+// 2 parts 44 / 41; 4096 rows 90 / 101 (256 x 256), 126 / 128 (128 x 128).
 ProductPlan product_plan(int M, int R, int Kp, bool wide, bool may_split) {
     struct Kind {
         ProductPlan::Kernel kernel;
         int a, b, most_rows;   // tile; rows up to which it is looked at
         float ends;            // direct kernels: their start, and the join of the waves
     };
-    static constexpr Kind kinds[] = {{ProductPlan::kDirect16, 16, 16, 32, 3.0f},   {ProductPlan::kDirect32, 16, 32, 64, 3.2f},
-                                     {ProductPlan::kDirect64, 32, 32, 256, 3.6f},  {ProductPlan::kDirect128, 32, 64, 512, 5.0f},
+    static constexpr Kind kinds[] = {{ProductPlan::kDirect16, 16, 16, 32, 2.5f},   {ProductPlan::kDirect32, 16, 32, 64, 2.8f},
+                                     {ProductPlan::kDirect64, 32, 32, 256, 3.6f},  {ProductPlan::kDirect128, 32, 64, 512, 4.1f},
                                      {ProductPlan::kTile64, 64, 64, 1024, 0},      {ProductPlan::kTile128, 128, 128, 1 << 30, 0},
                                      {ProductPlan::kTile256, 256, 256, 1 << 30, 0}};
     const int nkb = Kp / 128;
@@ -565,15 +580,15 @@ ProductPlan product_plan(int M, int R, int Kp, bool wide, bool may_split) {
             float t;
             if (k.kernel == ProductPlan::kTile256) {
                 const float full = std::min(mean, 1.0f);
-                t = std::ceil(mean) * (blocks * (1.63f + 0.27f * full) + 4.0f + 4.0f * full);
+                t = std::ceil(mean) * (blocks * (1.19f + 0.24f * full) + 6.3f + 3.5f * full);
             } else if (k.kernel == ProductPlan::kTile128) {
-                t = blocks * (wide ? std::max(1.05f, 0.95f * cu) : std::max(0.55f, 0.60f * cu)) + 4.0f * std::ceil(cu / 2);
+                t = blocks * (wide ? std::max(0.96f, 0.76f * cu) : std::max(0.51f, 0.47f * cu)) + 4.8f * std::ceil(cu / 2);
             } else if (k.kernel == ProductPlan::kTile64) {
-                t = blocks * (cu <= 1 ? 0.58f : 0.61f * cu) + 4.5f;
+                t = blocks * (cu <= 1 ? 0.58f : 0.53f * cu) + 4.7f;
             } else {
-                t = std::max(cu * blocks * ((k.a + k.b) * 128) / 34500.0f, 0.7f * ((blocks + 7) / 8)) + k.ends;
+                t = std::max(cu * blocks * ((k.a + k.b) * 128) / 33400.0f, 0.43f * ((blocks + 7) / 8)) + k.ends;
             }
-            if (parts > 1) t += 4.0f + static_cast<float>(parts) * R * M * 8 / 6.0e6f;
+            if (parts > 1) t += 2.3f + static_cast<float>(parts) * R * M * 8 / 4.65e6f;
             if (t < least) {
                 least = t;
                 best = {k.kernel, parts};
