@@ -52,7 +52,7 @@ struct ProductArgs {
 
 // How a product runs: which kernel, and into how many parts its reduction is split.
 struct ProductPlan {
-    enum Kernel { kDirect16, kDirect32, kDirect64, kDirect128, kTile64, kTile128, kTile256 };
+    enum Kernel { kDirect16, kDirect32, kDirect64, kTile64, kTile128x64, kTile128, kTile256 };
     Kernel kernel;
     int parts;
 };

@@ -531,8 +531,8 @@ static void variant(const ProductArgs &p, const ProductPlan &plan, hipStream_t s
             case ProductPlan::kDirect16: direct<1, 1, 8, ASC, BX, WIDE, OUT>(p, plan.parts, s); break;
             case ProductPlan::kDirect32: direct<1, 2, 8, ASC, BX, WIDE, OUT>(p, plan.parts, s); break;
             case ProductPlan::kDirect64: direct<2, 2, 8, ASC, BX, WIDE, OUT>(p, plan.parts, s); break;
-            case ProductPlan::kDirect128: direct<2, 4, 8, ASC, BX, WIDE, OUT>(p, plan.parts, s); break;
-            case ProductPlan::kTile64: direct<4, 4, 4, ASC, BX, WIDE, OUT>(p, plan.parts, s); break;
+            case ProductPlan::kTile64: tiled<2, 2, 2, 2, ASC, WIDE, OUT>(p, plan.parts, s); break;
+            case ProductPlan::kTile128x64: tiled<4, 2, 2, 2, ASC, WIDE, OUT>(p, plan.parts, s); break;
             case ProductPlan::kTile128: tiled<4, 4, 2, 2, ASC, WIDE, OUT>(p, plan.parts, s); break;
             case ProductPlan::kTile256:
                 if constexpr (!WIDE) tiled<8, 4, 2, 4, ASC, WIDE, OUT>(p, plan.parts, s);
@@ -544,29 +544,32 @@ static void variant(const ProductArgs &p, const ProductPlan &plan, hipStream_t s
 // Which kernel runs a product, and into how many parts its reduction is split: the least of their estimated
 // times.  The estimate is a workgroup's blocks times what one takes (in microseconds, fitted to times on this
 // card over ten weights, N from 512 to 8192, K from 512 to 18432, at 16 to 8192 rows, every kernel and split
-// of each: the rule's choice is 1.0 % above the best of them in the mean, 19 % at the worst), as often as its
-// workgroups outnumber the 256 CUs, plus each round's start and end, plus the join of the parts:
-//   direct kernels  the bytes of a block at 33.4 GB/s a CU (the waves of a CU share that rate), at least
-//                   0.43 for every 8 blocks: a small reduction is one round trip to memory
-//   64 x 64         0.58 a block alone on its CU, 0.53 shared, whatever the arithmetic
-//   128 x 128       0.51 alone, 0.47 shared by two; widened 0.96 and 0.76
-//   256 x 256       1.19 rising to 1.43 when every CU has one
-//   join            2.3 and the parts' bytes, written and read, at 4.65 TB/s
-// With M = 4096, K = 7168 (estimate / measured): 32 rows 13.1 / 13.1 (16 x 32 tiles), as 8 parts of 128 x 128
-// 12.5 / 13.0; 256 rows 21.5 / 19.8 (128 x 128, 4 parts), 2 parts 25 / 23.7; 777 rows 33 / 36,
-// 2 parts 44 / 41; 4096 rows 90 / 101 (256 x 256), 126 / 128 (128 x 128).
+// of each: the rule's choice is 0.8 % above the best of them in the mean, 18 % at the worst), as often as its
+// workgroups outnumber the 256 CUs, plus the start and end of each round, plus the join of the parts:
+//   direct kernels  the bytes of a block at 32.9 GB/s a CU (the waves of a CU share that rate), at least
+//                   0.5 for every 8 blocks: a small reduction is one round trip to memory
+//   tiled kernels   a block alone on its CU, and as a share of the CU's time; the second pair widened
+//   join            1.9 and the parts' bytes, written and read, at 5.4 TB/s
+// With M = 4096, K = 7168 (estimate / measured): 32 rows 10.6 / 12.1 (64 x 64, 8 parts), 16 x 32 direct
+// 13.5 / 13.1; 256 rows 19.5 / 20.1 (128 x 64, 2 parts), 128 x 128 in 4 parts 20.2 / 19.6; 777 rows 32 / 34
+// (128 x 128), 128 x 64 39 / 37; 4096 rows 89 / 99 (256 x 256), 128 x 128 121 / 128.
 ProductPlan product_plan(int M, int R, int Kp, bool wide, bool may_split) {
     struct Kind {
         ProductPlan::Kernel kernel;
         int a, b, most_rows;   // tile; rows up to which it is looked at
-        float ends;            // direct kernels: their start, and the join of the waves
+        float ends;            // start and end of a round
+        int round;             // tiled kernels: workgroups a CU holds at once
+        float alone, share, wide_alone, wide_share;
     };
-    static constexpr Kind kinds[] = {{ProductPlan::kDirect16, 16, 16, 32, 2.5f},   {ProductPlan::kDirect32, 16, 32, 64, 2.8f},
-                                     {ProductPlan::kDirect64, 32, 32, 256, 3.6f},  {ProductPlan::kDirect128, 32, 64, 512, 4.1f},
-                                     {ProductPlan::kTile64, 64, 64, 1024, 0},      {ProductPlan::kTile128, 128, 128, 1 << 30, 0},
-                                     {ProductPlan::kTile256, 256, 256, 1 << 30, 0}};
+    static constexpr Kind kinds[] = {{ProductPlan::kDirect16, 16, 16, 32, 2.7f},
+                                     {ProductPlan::kDirect32, 16, 32, 64, 3.0f},
+                                     {ProductPlan::kDirect64, 32, 32, 256, 4.0f},
+                                     {ProductPlan::kTile64, 64, 64, 1 << 30, 4.5f, 4, 0.27f, 0.19f, 0.37f, 0.30f},
+                                     {ProductPlan::kTile128x64, 128, 64, 1 << 30, 4.7f, 2, 0.35f, 0.31f, 0.55f, 0.53f},
+                                     {ProductPlan::kTile128, 128, 128, 1 << 30, 5.4f, 2, 0.48f, 0.44f, 0.87f, 0.78f},
+                                     {ProductPlan::kTile256, 256, 256, 1 << 30, 8.1f, 1, 0.97f, 1.40f}};
     const int nkb = Kp / 128;
-    if (nkb == 0) return {ProductPlan::kTile64, 1};   // no block: zeros are stored
+    if (nkb == 0) return {ProductPlan::kDirect64, 1};   // no block: zeros are stored
     ProductPlan best{ProductPlan::kTile128, 1};
     float least = 1e30f;
     for (const Kind &k : kinds) {
@@ -578,17 +581,16 @@ ProductPlan product_plan(int M, int R, int Kp, bool wide, bool may_split) {
             // workgroups of the fullest CU; behind the second round they even out
             const float mean = wgs * parts / 256.0f, cu = mean > 2 ? mean + 0.25f : std::ceil(mean);
             float t;
-            if (k.kernel == ProductPlan::kTile256) {
+            if (k.kernel == ProductPlan::kTile256) {   // fills a CU: whole rounds, and slower the fuller the card
                 const float full = std::min(mean, 1.0f);
-                t = std::ceil(mean) * (blocks * (1.19f + 0.24f * full) + 6.3f + 3.5f * full);
-            } else if (k.kernel == ProductPlan::kTile128) {
-                t = blocks * (wide ? std::max(0.96f, 0.76f * cu) : std::max(0.51f, 0.47f * cu)) + 4.8f * std::ceil(cu / 2);
-            } else if (k.kernel == ProductPlan::kTile64) {
-                t = blocks * (cu <= 1 ? 0.58f : 0.53f * cu) + 4.7f;
+                t = std::ceil(mean) * (blocks * (k.alone + (k.share - k.alone) * full) + k.ends + 2.5f * full);
+            } else if (k.round) {
+                t = blocks * (wide ? std::max(k.wide_alone, k.wide_share * cu) : std::max(k.alone, k.share * cu)) +
+                    k.ends * std::ceil(cu / k.round);
             } else {
-                t = std::max(cu * blocks * ((k.a + k.b) * 128) / 33400.0f, 0.43f * ((blocks + 7) / 8)) + k.ends;
+                t = std::max(cu * blocks * ((k.a + k.b) * 128) / 32900.0f, 0.5f * ((blocks + 7) / 8)) + k.ends;
             }
-            if (parts > 1) t += 2.3f + static_cast<float>(parts) * R * M * 8 / 4.65e6f;
+            if (parts > 1) t += 1.9f + static_cast<float>(parts) * R * M * 8 / 5.4e6f;
             if (t < least) {
                 least = t;
                 best = {k.kernel, parts};
