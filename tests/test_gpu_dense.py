@@ -197,6 +197,21 @@ def test_linear_many_rows(T, N, K):
         assert_product(y, want, mag, K, yd)
 
 
+@pytest.mark.parametrize("T,N,K", ((5, 144, 4112), (33, 144, 2064), (65, 144, 2064), (300, 144, 2064), (17, 4112, 4112),
+                                   (130, 2064, 4112), (200, 2064, 8208), (777, 1040, 8208)))
+def test_linear_split(T, N, K):
+    """Few tiles over a long reduction: several parts, for every tile; the last block and the last tile end early."""
+    r = rng(T, N, K, 13)
+    wt, w = weight(r, N, K)
+    xv, x = matrix(r, T, K, BF16, spread=1)
+    form, q = form_of(xv)
+    want, mag = q @ w.T, np.abs(q) @ np.abs(w).T
+    for yd in (BF16, F32):
+        y = run_linear(N, K, T, wt, form, ACT, yd)
+        assert_product(y, want, mag, K, yd)
+        assert torch.equal(y, run_linear(N, K, T, wt, x, BF16, yd))
+
+
 def test_linear_long_reduction():
     """K over 512 blocks, one and many rows."""
     r = rng(5)
@@ -276,6 +291,21 @@ def test_weight_grad_of_large_weights_and_long_batches(T, N, K):
         dw = torch.full((N, K), 3.0, dtype=TORCH[dt], device="cuda")
         ftm.ft_linear_weight_grad(N, K, T, dc, xc, dw)
         assert_product(dw, want, mag, T, dt)
+
+
+@pytest.mark.parametrize("T,N,K", ((130, 1040, 1040), (777, 1040, 1040), (5, 2064, 2064), (300, 2064, 4112)))
+def test_weight_grad_tiles(T, N, K):
+    r = rng(T, N, K, 14)
+    dyv, xv = matrix(r, T, N, BF16, spread=1)[0], matrix(r, T, K, BF16, spread=1)[0]
+    (dc, a), (xc, b) = form_of(dyv.T), form_of(xv.T)
+    want, mag = a @ b.T, np.abs(a) @ np.abs(b).T
+    for dt in (BF16, F32):
+        dw = torch.full((N + 1, K), 3.0, dtype=TORCH[dt], device="cuda")
+        ftm.ft_linear_weight_grad(N, K, T, dc, xc, dw)
+        assert torch.all(dw[N] == 3.0)
+        assert_product(dw[:N], want, mag, T, dt)
+    ftm.ft_linear_weight_grad(N, K, T, dc, xc, dw, accumulate=True)
+    assert_product(dw[:N], 2 * want, 2 * mag, T + 1, F32)
 
 
 def test_weight_grad_without_tokens():
