@@ -438,7 +438,10 @@ __global__ __launch_bounds__(256) void router_grad(BalanceArgs b, int run) {
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-            for (int i = 0; i < L::NE; ++i) d[i] = a[i] * gate[L::expert(sub, i)];
+            for (int i = 0; i < L::NE; ++i) {
+                const float q = gate[L::expert(sub, i)];
+                d[i] = q == 0.0f ? 0.0f : a[i] * q;   // a padding token's logits may be anything
+            }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         } else {
 #pragma unroll

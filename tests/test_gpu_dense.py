@@ -439,6 +439,34 @@ def test_router_far_and_infinite_logits(gating):
         assert np.all(np.abs(f64(d) - want) <= 2e-5 * mag + 1e-30)
 
 
+@pytest.mark.parametrize("gating", (oracle.GATE_SOFTMAX, oracle.GATE_SIGMOID))
+def test_router_padding_that_is_not_finite(gating):
+    """Masked tokens whose logits are NaN or infinite change nothing, and their rows of the gradient are zeros
+    where the gates' gradients are."""
+    r = rng(15, gating)
+    for T, E in ((40, 48), (700, 200)):
+        desc = {"n_experts": E, "top_k": 3, "gating": gating, "n_seq": 2, "coef": 1.0}
+        logits, ids, off, _ = router_case(r, T, E, 3, 2, False)
+        mask = (r.random(T) < 0.7).astype(np.uint8)
+        mask[:2] = 1, 0
+        bad = logits.copy()
+        bad[mask == 0] = r.choice(np.float32([np.nan, np.inf, -np.inf, 3e38]), size=(int((mask == 0).sum()), E))
+        gates = r.random((T, 3)).astype(np.float32)
+        dw = (r.normal(size=(T, 3)) * mask[:, None]).astype(np.float32)
+        grads = []
+        for l in (logits, bad):
+            out, args = check_balance(desc, logits, ids, off, mask)
+            again = ftm.BalanceBuffers(2, E)
+            ftm.ft_balance_loss(desc, cuda(l), cuda(ids), T, again, ftm.alloc_balance_workspace(desc, T), **args)
+            for n in ("counts", "tokens", "prob", "frac", "loss"):
+                assert torch.equal(getattr(out, n), getattr(again, n))
+            d = torch.empty(T, E, device="cuda")
+            ftm.ft_router_backward(desc, cuda(l), cuda(ids), T, out, torch.ones(2, device="cuda"), d, topk_w=cuda(gates),
+                                   d_topk_w=cuda(dw), **args)
+            grads.append(d)
+        assert torch.equal(*grads) and not grads[0][torch.from_numpy(mask == 0).cuda()].any()
+
+
 def test_balance_edges():
     """No tokens, empty sequences, a mask that leaves a sequence nothing, ids outside the experts, and
     one sequence without offsets."""
