@@ -13,8 +13,13 @@
 // the launches' latency.  Up to 128 experts a token is held by one 16-lane row of a wave, whose reductions need
 // no step across rows and serve four tokens at once, above by the whole wave (256 experts in a row take 138
 // registers: backward 49.8 us against 48.5 for 65536 tokens).  The next token is requested before the current
-// one is worked on (33.5 us; the copy of as much takes 25.5).  The sums over tokens stay in the lanes' registers.  Every sum is in float32 in a fixed
-// order: the results are the same in every run.
+// one is worked on: 65536 tokens of 256 experts backward 34.7 us, 4.1 TB/s (a copy of as much 25.5; the vector unit
+// works half of the time).  The sums over tokens stay in the lanes' registers.  Every sum is in float32 in a
+// fixed order: the results are the same in every run.
+//
+// Forward: up to 512 tokens one launch, a workgroup per sequence (48 tokens of 128 experts 4.5 us); above, parts of the
+// tokens over up to 256 workgroups and a join (8192 tokens of 256 experts in 9 sequences 12.6 us: two launches,
+// each some round trips to memory long).
 #include "ftmoe_device.h"
 #include "ftmoe_internal.h"
 
@@ -329,18 +334,23 @@ __global__ __launch_bounds__(kBalThreads) void balance_join(BalanceArgs b) {
     int count = 0;
     if (beg < end) {
         const int q0 = beg / b.part_tokens, q1 = (end - 1) / b.part_tokens;
-        if (e < b.E) {
-#pragma unroll 8
-            for (int q = q0 + side; q <= q1; q += kSide) {
-                const size_t o = (static_cast<size_t>(q) + s) * b.E + e;
-                const float2 v = b.ws_sums[o];
-                prob += v.x;
-                count += __float_as_int(v.y);
+        static_assert(kBalMaxParts <= kBalThreads, "one part a thread");
+        const int n = b.ws_tokens[min(q0 + t, q1) + s];
+        // eight rows on the way at a time; behind the last one it again, unused
+        constexpr int kAhead = 8;
+        if (e < b.E)
+            for (int q = q0 + side; q <= q1; q += kAhead * kSide) {
+                float2 v[kAhead];
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) v[i] = b.ws_sums[(static_cast<size_t>(min(q + i * kSide, q1)) + s) * b.E + e];
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i)
+                    if (q + i * kSide <= q1) {
+                        prob += v[i].x;
+                        count += __float_as_int(v[i].y);
+                    }
             }
-        }
-        int n = 0;
-        for (int q = q0 + t; q <= q1; q += kBalThreads) n += b.ws_tokens[q + s];
-        if (n) atomicAdd(&s_tokens, n);
+        if (q0 + t <= q1 && n) atomicAdd(&s_tokens, n);
     }
     s_prob[side][e] = prob;
     s_count[side][e] = count;
