@@ -40,6 +40,7 @@ tensors.  A non-OK status raises FtError.  If the library is not built, importin
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -684,7 +685,9 @@ def ft_prefill_layers(desc: dict, host_layers: list, dev_bufs: list, slot_table:
 # ------------------------------------------------------------ dense layers next to the experts
 
 _FLOATS = {torch.float32: FT_DT_F32, torch.bfloat16: FT_DT_BF16}
+_FLOAT_TYPES = tuple(_FLOATS)
 _CODES = (torch.uint8, torch.float8_e4m3fn)
+_BYTES, _F32, _I32, _MASKS = (torch.uint8,), (torch.float32,), (torch.int32,), (torch.uint8, torch.bool)
 
 
 def _pad128(n: int) -> int:
@@ -712,29 +715,27 @@ class ActCodes:
     def c(self) -> ft_act_codes_t:
         return ft_act_codes_t(_ptr(self.codes), _ptr(self.scales))
 
-    def get_device(self) -> int:
-        if self.codes.get_device() != self.scales.get_device():
-            raise ValueError("codes and scales on two devices")
-        return self.codes.get_device()
 
-
-def _device_of(*tensors) -> int:
-    """Index of the one device that holds the call's tensors."""
-    dev = -1
-    for t in tensors:
-        if t is None:
-            continue
-        d = t.get_device()
-        if d != dev:
-            if dev >= 0:
-                raise ValueError(f"tensors on devices {dev} and {d}; a call works on one device")
-            dev = d
-    return dev
+def _arg(dev: int, t, name: str, dtypes: tuple, numel: int):
+    """The checks of _need, contiguity and one device for the whole call (``dev``: the one so far, -1 before the
+    first), in one frame per tensor: at a call's few microseconds they count.  -> (device, address)."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.numel() < numel:
+        _need(t, name, dtypes, numel)
+    d = t.get_device()
+    if d != dev or d < 0:
+        if d < 0:
+            raise ValueError(f"{name}: must be a device (cuda) tensor")
+        if dev >= 0:
+            raise ValueError(f"{name}: tensors on devices {dev} and {d}; a call works on one device")
+    if not t.is_contiguous():
+        raise ValueError("tensors passed to libftmoe must be contiguous")
+    return d, t.data_ptr()
 
 
 # a torch.cuda.Stream object costs a call more than its kernel's launch does
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _on(device: int, call, *args) -> int:
@@ -742,24 +743,30 @@ def _on(device: int, call, *args) -> int:
     None for that device's current one."""
     stream = args[-1]
     stream = _raw_stream(device) if stream is None else _stream(stream)
-    if device == torch.cuda.current_device():
+    if device == _current_device():
         return call(*args[:-1], stream)
     with torch.cuda.device(device):
         return call(*args[:-1], stream)
 
 
-def _need_codes(c, name: str, rows: int, cols: int) -> None:
+def _need_codes(c, name: str, rows: int, cols: int, dev: int = -1):
+    """The 8-bit form of a rows x cols matrix.  -> (device, address of codes, of scales)."""
     if not isinstance(c, ActCodes):
         raise ValueError(f"{name}: expected an ActCodes, got {type(c).__name__}")
     if c.rows != rows or c.cols != cols:
         raise ValueError(f"{name}: the form of a {c.rows} x {c.cols} matrix, the call needs {rows} x {cols}")
     kp = _pad128(cols)
-    _need(c.codes, f"{name}.codes", _CODES, rows * kp)
-    _need(c.scales, f"{name}.scales", torch.uint8, kp // 128 * _pad128(rows))
+    dev, codes = _arg(dev, c.codes, name + ".codes", _CODES, rows * kp)
+    dev, scales = _arg(dev, c.scales, name + ".scales", _BYTES, kp // 128 * _pad128(rows))
+    return dev, codes, scales
 
 
-def _ref(c):
-    return None if c is None else ctypes.byref(c.c())
+def _codes_arg(dev: int, c, name: str, rows: int, cols: int, optional: bool = False):
+    """-> (device, the ft_act_codes_t to pass); None passes as NULL where the call may leave the form out."""
+    if c is None and optional:
+        return dev, None
+    dev, codes, scales = _need_codes(c, name, rows, cols, dev)
+    return dev, ctypes.byref(ft_act_codes_t(codes, scales))
 
 
 def _need_sizes(T: int, *features: int) -> None:
@@ -774,18 +781,20 @@ def ft_act_quantize(x: torch.Tensor, T: int, C: int, row: Optional[ActCodes] = N
     _need_sizes(T, C)
     if T == 0:
         return
-    _need(x, "x", tuple(_FLOATS), T * C)
-    if row is not None:
-        _need_codes(row, "row", T, C)
-    if col is not None:
-        _need_codes(col, "col", C, T)
-    st = _on(_device_of(x, row, col), load().ft_act_quantize, _ptr(x), _FLOATS[x.dtype], T, C, _ref(row), _ref(col),
-             stream)
+    dev, xp = _arg(-1, x, "x", _FLOAT_TYPES, T * C)
+    dev, rp = _codes_arg(dev, row, "row", T, C, True)
+    dev, cp = _codes_arg(dev, col, "col", C, T, True)
+    st = _on(dev, load().ft_act_quantize, xp, _FLOATS[x.dtype], T, C, rp, cp, stream)
     _check(st, "ft_act_quantize")
 
 
+@functools.lru_cache(maxsize=256)   # a struct per set of values
+def _linear_struct(*values: int) -> ft_linear_desc_t:
+    return ft_linear_desc_t(*values)
+
+
 def _linear_desc(d: dict) -> ft_linear_desc_t:
-    return ft_linear_desc_t(int(d["out_features"]), int(d["in_features"]), int(d["x_dtype"]), int(d["y_dtype"]))
+    return _linear_struct(int(d["out_features"]), int(d["in_features"]), int(d["x_dtype"]), int(d["y_dtype"]))
 
 
 def ft_linear_workspace_bytes(desc: dict, max_tokens: int) -> int:
@@ -800,10 +809,11 @@ def alloc_linear_workspace(desc: dict, max_tokens: int, device="cuda") -> torch.
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def _need_weight(weight: dict, name: str, N: int, K: int) -> None:
+def _weight_args(dev: int, weight: dict, name: str, N: int, K: int):
     kp = _pad128(K)
-    _need(weight.get("w"), f"{name}['w']", _CODES, N * kp)
-    _need(weight.get("s"), f"{name}['s']", torch.float32, _pad128(N) // 128 * (kp // 128))
+    dev, w = _arg(dev, weight.get("w"), name + "['w']", _CODES, N * kp)
+    dev, s = _arg(dev, weight.get("s"), name + "['s']", _F32, _pad128(N) // 128 * (kp // 128))
+    return dev, w, s
 
 
 def ft_linear(desc: dict, weight: dict, x, T: int, y: torch.Tensor, ws: Optional[torch.Tensor] = None,
@@ -815,34 +825,31 @@ def ft_linear(desc: dict, weight: dict, x, T: int, y: torch.Tensor, ws: Optional
     _need_sizes(T, N, K)
     if T == 0:
         return
-    _need_weight(weight, "weight", N, K)
+    dev, w, scales = _weight_args(-1, weight, "weight", N, K)
     if d.x_dtype == FT_DT_FP8_ACT:
-        _need_codes(x, "x", T, K)
-        xp, xs = x.codes, x.scales
-        if ws is not None:
-            _need(ws, "ws", torch.uint8, 0)
+        dev, xp, xs = _need_codes(x, "x", T, K, dev)
     else:
         if d.x_dtype not in _X_DTYPES:
             raise FtError(FT_ERR_DTYPE, "ft_linear")
-        _need(x, "x", _X_DTYPES[d.x_dtype], T * K)
-        _need(ws, "ws", torch.uint8, 0)
-        xp, xs = x, None
+        dev, xp = _arg(dev, x, "x", (_X_DTYPES[d.x_dtype],), T * K)
+        xs = None
     if d.y_dtype not in _X_DTYPES:
         raise FtError(FT_ERR_DTYPE, "ft_linear")
-    _need(y, "y", _X_DTYPES[d.y_dtype], T * N)
-    w, s = weight["w"], weight["s"]
-    st = _on(_device_of(w, s, xp, xs, y, ws), load().ft_linear, ctypes.byref(d), _ptr(w), _ptr(s), _ptr(xp), _ptr(xs), T,
-             _ptr(y), _ptr(ws), 0 if ws is None else ws.numel(), stream)
+    dev, yp = _arg(dev, y, "y", (_X_DTYPES[d.y_dtype],), T * N)
+    wp, room = None, 0
+    if ws is not None or d.x_dtype != FT_DT_FP8_ACT:
+        dev, wp = _arg(dev, ws, "ws", _BYTES, 0)
+        room = ws.numel()
+    st = _on(dev, load().ft_linear, ctypes.byref(d), w, scales, xp, xs, T, yp, wp, room, stream)
     _check(st, "ft_linear")
 
 
 def ft_linear_transpose(out_features: int, in_features: int, weight: dict, weight_t: dict, stream=None) -> None:
     N, K = int(out_features), int(in_features)
     _need_sizes(0, N, K)
-    _need_weight(weight, "weight", N, K)
-    _need_weight(weight_t, "weight_t", K, N)
-    t = (weight["w"], weight["s"], weight_t["w"], weight_t["s"])
-    st = _on(_device_of(*t), load().ft_linear_transpose, N, K, *map(_ptr, t), stream)
+    dev, w, scales = _weight_args(-1, weight, "weight", N, K)
+    dev, wt, scales_t = _weight_args(dev, weight_t, "weight_t", K, N)
+    st = _on(dev, load().ft_linear_transpose, N, K, w, scales, wt, scales_t, stream)
     _check(st, "ft_linear_transpose")
 
 
@@ -851,14 +858,12 @@ def ft_linear_weight_grad(out_features: int, in_features: int, T: int, dy_col: A
     """``dw``: float32 or bfloat16 [out_features][in_features]."""
     N, K, T = int(out_features), int(in_features), int(T)
     _need_sizes(T, N, K)
-    _need(dw, "dw", tuple(_FLOATS), N * K)
+    dev, out = _arg(-1, dw, "dw", _FLOAT_TYPES, N * K)
+    yp = xp = None
     if T > 0:
-        _need_codes(dy_col, "dy_col", N, T)
-        _need_codes(x_col, "x_col", K, T)
-    else:
-        dy_col = x_col = None
-    st = _on(_device_of(dw, dy_col, x_col), load().ft_linear_weight_grad, N, K, T, _ref(dy_col), _ref(x_col), _ptr(dw),
-             _FLOATS[dw.dtype], 1 if accumulate else 0, stream)
+        dev, yp = _codes_arg(dev, dy_col, "dy_col", N, T)
+        dev, xp = _codes_arg(dev, x_col, "x_col", K, T)
+    st = _on(dev, load().ft_linear_weight_grad, N, K, T, yp, xp, out, _FLOATS[dw.dtype], 1 if accumulate else 0, stream)
     _check(st, "ft_linear_weight_grad")
 
 
@@ -874,12 +879,10 @@ def ft_swiglu_quantize(gu: torch.Tensor, T: int, inter: int, h: ActCodes, saved:
     _need_inter(T, I)
     if T == 0:
         return
-    _need(gu, "gu", tuple(_FLOATS), T * 2 * I)
-    _need_codes(h, "h", T, I)
-    if saved is not None:
-        _need_codes(saved, "saved", T, 2 * I)
-    st = _on(_device_of(gu, h, saved), load().ft_swiglu_quantize, _ptr(gu), _FLOATS[gu.dtype], T, I, _ref(h), _ref(saved),
-             stream)
+    dev, gp = _arg(-1, gu, "gu", _FLOAT_TYPES, T * 2 * I)
+    dev, hp = _codes_arg(dev, h, "h", T, I)
+    dev, sp = _codes_arg(dev, saved, "saved", T, 2 * I, True)
+    st = _on(dev, load().ft_swiglu_quantize, gp, _FLOATS[gu.dtype], T, I, hp, sp, stream)
     _check(st, "ft_swiglu_quantize")
 
 
@@ -889,13 +892,12 @@ def ft_swiglu_backward(saved: ActCodes, dh: torch.Tensor, T: int, inter: int, dg
     _need_inter(T, I)
     if T == 0:
         return
-    _need_codes(saved, "saved", T, 2 * I)
-    _need(dh, "dh", tuple(_FLOATS), T * I)
-    for c, name, rows, cols in ((dgu_row, "dgu_row", T, 2 * I), (dgu_col, "dgu_col", 2 * I, T), (h_col, "h_col", I, T)):
-        if c is not None:
-            _need_codes(c, name, rows, cols)
-    st = _on(_device_of(saved, dh, dgu_row, dgu_col, h_col), load().ft_swiglu_backward, _ref(saved), _ptr(dh),
-             _FLOATS[dh.dtype], T, I, _ref(dgu_row), _ref(dgu_col), _ref(h_col), stream)
+    dev, sp = _codes_arg(-1, saved, "saved", T, 2 * I)
+    dev, dp = _arg(dev, dh, "dh", _FLOAT_TYPES, T * I)
+    dev, rp = _codes_arg(dev, dgu_row, "dgu_row", T, 2 * I, True)
+    dev, cp = _codes_arg(dev, dgu_col, "dgu_col", 2 * I, T, True)
+    dev, hp = _codes_arg(dev, h_col, "h_col", I, T, True)
+    st = _on(dev, load().ft_swiglu_backward, sp, dp, _FLOATS[dh.dtype], T, I, rp, cp, hp, stream)
     _check(st, "ft_swiglu_backward")
 
 
@@ -921,9 +923,14 @@ class BalanceBuffers:
         return ft_balance_t(*[_ptr(getattr(self, n)) for n, _ in ft_balance_t._fields_])
 
 
+@functools.lru_cache(maxsize=256)
+def _balance_struct(*values) -> ft_balance_desc_t:
+    return ft_balance_desc_t(*values)
+
+
 def _balance_desc(d: dict) -> ft_balance_desc_t:
-    return ft_balance_desc_t(int(d["n_experts"]), int(d["top_k"]), int(d["gating"]), int(d["n_seq"]),
-                             float(d.get("coef", 1.0)))
+    return _balance_struct(int(d["n_experts"]), int(d["top_k"]), int(d["gating"]), int(d["n_seq"]),
+                           float(d.get("coef", 1.0)))
 
 
 def ft_balance_workspace_bytes(desc: dict, max_tokens: int) -> int:
@@ -937,25 +944,32 @@ def alloc_balance_workspace(desc: dict, max_tokens: int, device="cuda") -> torch
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def _need_tokens(d: ft_balance_desc_t, logits, topk_ids, T: int, seq_off, mask) -> None:
+def _token_args(d: ft_balance_desc_t, logits, topk_ids, T: int, seq_off, mask):
+    """-> (device, addresses of logits, topk_ids, seq_off, mask)."""
     if T < 0:
         raise FtError(FT_ERR_SHAPE, "sizes")
+    dev, lp, ip, sp, mp = -1, None, None, None, None
     if T > 0:
-        _need(logits, "logits", torch.float32, T * d.n_experts)
+        dev, lp = _arg(dev, logits, "logits", _F32, T * d.n_experts)
         if topk_ids is not None:
-            _need(topk_ids, "topk_ids", torch.int32, T * d.top_k)
+            dev, ip = _arg(dev, topk_ids, "topk_ids", _I32, T * d.top_k)
         if mask is not None:
-            _need(mask, "mask", (torch.uint8, torch.bool), T)
+            dev, mp = _arg(dev, mask, "mask", _MASKS, T)
     if seq_off is not None:
-        _need(seq_off, "seq_off", torch.int32, d.n_seq + 1)
+        dev, sp = _arg(dev, seq_off, "seq_off", _I32, d.n_seq + 1)
+    return dev, lp, ip, sp, mp
 
 
-def _need_balance(d: ft_balance_desc_t, b, names) -> None:
+def _balance_arg(dev: int, d: ft_balance_desc_t, b, names):
+    """The buffers ``names`` of a BalanceBuffers as an ft_balance_t, the others left out."""
     if not isinstance(b, BalanceBuffers):
         raise ValueError("expected a BalanceBuffers")
+    out = ft_balance_t()
     for n in names:
-        _need(getattr(b, n), n, torch.int32 if n in ("counts", "tokens") else torch.float32,
-              d.n_seq * (1 if n in ("tokens", "loss") else d.n_experts))
+        dev, at = _arg(dev, getattr(b, n), n, _I32 if n in ("counts", "tokens") else _F32,
+                       d.n_seq * (1 if n in ("tokens", "loss") else d.n_experts))
+        setattr(out, n, at)
+    return dev, ctypes.byref(out)
 
 
 def ft_balance_loss(desc: dict, logits: torch.Tensor, topk_ids: torch.Tensor, T: int, out: BalanceBuffers,
@@ -965,13 +979,10 @@ def ft_balance_loss(desc: dict, logits: torch.Tensor, topk_ids: torch.Tensor, T:
     d, T = _balance_desc(desc), int(T)
     if T > 0 and topk_ids is None:
         raise ValueError("topk_ids: required")
-    _need_tokens(d, logits, topk_ids, T, seq_off, mask)
-    _need_balance(d, out, ("counts", "tokens", "prob", "frac", "loss"))
-    _need(ws, "ws", torch.uint8, 0)
-    o = out.c()
-    st = _on(_device_of(out.loss, logits, topk_ids, seq_off, mask, out.counts, out.tokens, out.prob, out.frac, ws),
-             load().ft_balance_loss, ctypes.byref(d), _ptr(logits), _ptr(topk_ids), T, _ptr(seq_off), _ptr(mask),
-             ctypes.byref(o), _ptr(ws), ws.numel(), stream)
+    dev, lp, ip, sp, mp = _token_args(d, logits, topk_ids, T, seq_off, mask)
+    dev, bp = _balance_arg(dev, d, out, ("counts", "tokens", "prob", "frac", "loss"))
+    dev, wp = _arg(dev, ws, "ws", _BYTES, 0)
+    st = _on(dev, load().ft_balance_loss, ctypes.byref(d), lp, ip, T, sp, mp, bp, wp, ws.numel(), stream)
     _check(st, "ft_balance_loss")
 
 
@@ -981,22 +992,18 @@ def ft_router_backward(desc: dict, logits: torch.Tensor, topk_ids: Optional[torc
                        seq_off: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None, stream=None) -> None:
     """``balance`` and ``d_loss`` may be None (gates only), or ``d_topk_w`` (loss only)."""
     d, T = _balance_desc(desc), int(T)
-    _need_tokens(d, logits, topk_ids, T, seq_off, mask)
+    dev, lp, ip, sp, mp = _token_args(d, logits, topk_ids, T, seq_off, mask)
     if T == 0:
         return
-    _need(d_logits, "d_logits", torch.float32, T * d.n_experts)
-    b, used = ft_balance_t(), ()
+    dev, op = _arg(dev, d_logits, "d_logits", _F32, T * d.n_experts)
+    bp = dl = wp = dw = None
     if d_loss is not None:
-        _need(d_loss, "d_loss", torch.float32, d.n_seq)
-        _need_balance(d, balance, ("tokens", "frac"))
-        used = (balance.tokens, balance.frac)
-        b.tokens, b.frac = map(_ptr, used)
+        dev, dl = _arg(dev, d_loss, "d_loss", _F32, d.n_seq)
+        dev, bp = _balance_arg(dev, d, balance, ("tokens", "frac"))
     if d_topk_w is not None:
         if topk_ids is None:
             raise ValueError("topk_ids: required with d_topk_w")
-        _need(topk_w, "topk_w", torch.float32, T * d.top_k)
-        _need(d_topk_w, "d_topk_w", torch.float32, T * d.top_k)
-    st = _on(_device_of(logits, topk_ids, d_logits, d_loss, topk_w, d_topk_w, seq_off, mask, *used),
-             load().ft_router_backward, ctypes.byref(d), _ptr(logits), _ptr(topk_ids), T, _ptr(seq_off), _ptr(mask),
-             ctypes.byref(b), _ptr(d_loss), _ptr(topk_w), _ptr(d_topk_w), _ptr(d_logits), stream)
+        dev, wp = _arg(dev, topk_w, "topk_w", _F32, T * d.top_k)
+        dev, dw = _arg(dev, d_topk_w, "d_topk_w", _F32, T * d.top_k)
+    st = _on(dev, load().ft_router_backward, ctypes.byref(d), lp, ip, T, sp, mp, bp, dl, wp, dw, op, stream)
     _check(st, "ft_router_backward")
