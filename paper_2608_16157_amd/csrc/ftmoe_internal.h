@@ -403,10 +403,11 @@ hipError_t launch_weight_transpose(const uint8_t *w, const float *s, uint8_t *wt
 // ws: room for the parts of a split reduction, or null
 hipError_t launch_product(const ProductArgs &p, bool a_e8m0, int bx, int out, float *ws, hipStream_t s);
 // Rows, and bytes of their codes, up to which a product quantises its input itself.  Every workgroup then
-// does that for all rows: with K = 7168 1 row takes 8.3 us against 9.6 with a launch of its own, 2 rows 9.4
-// against 9.8, 4 rows 11.1 against 10.1; with K = 2048 8 rows 8.1 against 8.4, 12 rows 9.6 against 8.7.
+// does that for all rows (in this order: itself, with a launch of its own).  4096 x 7168: 1 row 7.7 / 9.6 us,
+// 4 rows 9.8 / 12.9; 2048 x 4096: 6 rows 7.0 / 9.1, 8 rows 8.0 / 9.2; 512 x 7168: 3 rows 7.3 / 7.6, 4 rows 8.1 / 7.9;
+// 7168 x 2048: 12 rows 8.1 / 8.7, 16 rows 9.6 / 9.2.
 constexpr int kDirectTokens = 16;
-constexpr int kDirectBytes = 20 * 1024;
+constexpr int kDirectBytes = 32 * 1024;
 constexpr int kBalWholeTokens = 512;   // tokens up to which one launch sums each sequence in one workgroup
 constexpr int kBalMaxParts = 256;      // beyond: parts of the tokens, one workgroup each, and their join
 constexpr int kBalMinPart = 32;
