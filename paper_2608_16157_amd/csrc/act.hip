@@ -10,7 +10,7 @@
 // The column form needs a maximum over 128 rows and the transposed codes: a workgroup owns a tile of
 // 128 x 128 elements, each thread a patch of 4 rows x 8 columns, so that the codes of 4 rows of a column
 // leave as one word through LDS and both forms store whole 128-byte lines.  Both forms of 8192 x 7168:
-// 43 us, 5.4 TB/s.  SwiGLU backward, three such planes at 9 bytes a channel: 8192 x 2048 in 38 us, 4.0 TB/s; the
+// 40 us, 5.9 TB/s.  SwiGLU backward, three such planes at 9 bytes a channel: 8192 x 2048 in 38 us, 4.0 TB/s; the
 // vector unit works 0.4 of that, and with two tiles a CU (128 registers a thread) its work and the loads
 // overlap only between those two.  A tile after the other by the same workgroup, the next one's loads on the
 // way, spills registers and is slower.

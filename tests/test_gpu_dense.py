@@ -643,3 +643,97 @@ def test_router_step_after_the_layer_call():
         step()
         torch.cuda.synchronize()
         assert torch.equal(got[0], d) and torch.equal(got[1], out.loss)
+
+
+def test_calls_with_workspaces_captured_and_at_once():
+    """Few rows, a split reduction, and the balance loss in parts, with their workspaces: captured and replayed with
+    new inputs and eager work between the replays, and on two streams at once, every result the eager call's bits."""
+    r = rng(23)
+    N, K, E, k, n_seq, Tb = 528, 4112, 48, 4, 5, 2000
+    wt, _ = weight(r, N, K)
+    desc = lambda xd: {"out_features": N, "in_features": K, "x_dtype": xd, "y_dtype": BF16}
+    bal = {"n_experts": E, "top_k": k, "gating": 1, "n_seq": n_seq, "coef": 0.5}
+    off = cuda(np.array([0, 400, 400, 900, 1700, 1900], np.int32))
+
+    def state():
+        return {"few": torch.empty(3, K, dtype=torch.bfloat16, device="cuda"), "many": torch.empty(150, K, dtype=torch.bfloat16, device="cuda"),
+                "logits": torch.empty(Tb, E, device="cuda"), "ids": torch.empty(Tb, k, dtype=torch.int32, device="cuda"),
+                "y3": torch.zeros(3, N, dtype=torch.bfloat16, device="cuda"), "y150": torch.zeros(150, N, dtype=torch.bfloat16, device="cuda"),
+                "d": torch.zeros(Tb, E, device="cuda"), "out": ftm.BalanceBuffers(n_seq, E), "one": torch.ones(n_seq, device="cuda"),
+                "ws": ftm.alloc_linear_workspace(desc(BF16), 150), "bws": ftm.alloc_balance_workspace(bal, Tb)}
+
+    def fill(s, seed):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        for n in ("few", "many", "logits"):
+            s[n].normal_(generator=g)
+        s["ids"].copy_(s["logits"].topk(k, dim=1).indices)
+
+    def run(s):
+        ftm.ft_linear(desc(BF16), wt, s["few"], 3, s["y3"], s["ws"])
+        ftm.ft_linear(desc(BF16), wt, s["many"], 150, s["y150"], s["ws"])
+        ftm.ft_balance_loss(bal, s["logits"], s["ids"], Tb, s["out"], s["bws"], seq_off=off)
+        ftm.ft_router_backward(bal, s["logits"], None, Tb, s["out"], s["one"], s["d"], seq_off=off)
+
+    results = lambda s: [s["y3"], s["y150"], s["d"], s["out"].loss, s["out"].counts, s["out"].frac]
+    a, b = state(), state()
+    fill(a, 0)
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        run(a)
+    for seed in (1, 2, 3):
+        fill(a, seed)
+        graph.replay()
+        fill(b, seed)
+        run(b)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(results(a), results(b)))
+    want = [[t.clone() for t in results(b)]]
+    fill(a, 4)
+    run(a)
+    want.append([t.clone() for t in results(a)])
+    for s in (a, b):
+        for t in results(s):
+            t.zero_()
+    torch.cuda.synchronize()
+    other = torch.cuda.Stream()
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            run(b)
+        with torch.cuda.stream(other):
+            run(a)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(results(b), want[0]))
+    assert all(torch.equal(x, y) for x, y in zip(results(a), want[1]))
+
+
+def test_offsets_past_32_bits():
+    """1048576 tokens, all zeros but the last 384: codes, results and inputs past 4 GiB, in every form and product.
+    Rows of zeros add exact zeros to a sum, so the bounds are those of 384 terms."""
+    T, L, N, K = 1048576, 384, 2064, 4112
+    r = rng(24)
+    wt, w = weight(r, N, K)
+    xv, xl = matrix(r, L, K, BF16, spread=1)
+    dv, dl = matrix(r, L, N, BF16, spread=1)
+    x, dy = torch.zeros(T, K, dtype=torch.bfloat16, device="cuda"), torch.zeros(T, N, dtype=torch.bfloat16, device="cuda")
+    x[-L:], dy[-L:] = xl, dl
+    row, xc, dc = ftm.ActCodes(T, K), ftm.ActCodes(K, T), ftm.ActCodes(N, T)
+    ftm.ft_act_quantize(x, T, K, row, xc)
+    ftm.ft_act_quantize(dy, T, N, col=dc)
+    del x, dy
+    codes, scales = dense.quantize(xv)
+    assert np.array_equal(row.codes[-L:].cpu().numpy(), codes) and np.array_equal(row.scales[:, -L:].cpu().numpy(), scales[:, :L])
+    assert not row.codes[:-L].any()
+    for c, v in ((xc, xv), (dc, dv)):
+        codes, scales = dense.quantize(v.T)
+        assert np.array_equal(c.codes[:, -L:].cpu().numpy(), codes)
+        assert np.array_equal(c.scales[-L // 128:, :v.shape[1]].cpu().numpy(), scales[:, :v.shape[1]])
+    q, a, b = form_of(xv)[1], form_of(dv.T)[1], form_of(xv.T)[1]
+    y = torch.full((T, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    ftm.ft_linear({"out_features": N, "in_features": K, "x_dtype": ACT, "y_dtype": BF16}, wt, row, T, y)
+    assert_product(y[-L:], q @ w.T, np.abs(q) @ np.abs(w).T, K, BF16)
+    assert not y[:-L].any()
+    for dt in (BF16, F32):
+        dw = torch.empty(N, K, dtype=TORCH[dt], device="cuda")
+        ftm.ft_linear_weight_grad(N, K, T, dc, xc, dw)
+        assert_product(dw, a @ b.T, np.abs(a) @ np.abs(b).T, L, dt)
