@@ -5,7 +5,7 @@
 // All of these move memory once and compute little: the bound is HBM.
 //
 // The row form alone: 8 lanes per row and block of 128, 16 values a lane, so a block's maximum needs only
-// rotations within a lane row and no LDS.  8192 x 7168 bf16: 31 us, 5.7 TB/s.
+// rotations within a lane row and no LDS.  8192 x 7168 bf16: 29 us, 6.05 TB/s.
 //
 // The column form needs a maximum over 128 rows and the transposed codes: a workgroup owns a tile of
 // 128 x 128 elements, each thread a patch of 4 rows x 8 columns, so that the codes of 4 rows of a column
@@ -202,7 +202,7 @@ hipError_t launch_act_quantize(const void *x, bool f32, int T, int C, const ActF
 }
 
 // SwiGLU forward: h = silu(g) u from gu [T][2 I] (gate columns first), h in the row form and, if asked for,
-// gu itself.  8 lanes per (matrix row, block of 128 channels of h).
+// gu itself.  8 lanes per (matrix row, block of 128 channels of h).  Bound: HBM; 8192 x 2048 in 20 us, 5.8 TB/s.
 template <class XT>
 __global__ __launch_bounds__(256) void swiglu_quantize(const XT *gu, int T, int I, ActForm h, ActForm saved) {
     const int sub = threadIdx.x % 8, kb = blockIdx.x, nkb = I / 128;
