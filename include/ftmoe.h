@@ -513,7 +513,8 @@ ft_status_t ft_act_quantize(const void *x, int32_t x_dtype, int32_t T, int32_t C
  * experts' format and activations in 8 bits (a shared expert's or a dense layer's projections).
  *   w         [N][Kp] e4m3fn codes (Kp as above; codes of the padding columns 0; for K a multiple
  *             of 128 a bank row of ft_banks_t), w_scales [ceil(N/128)][Kp/128] float32:
- *             weight (r, c) = code(r, c) * scale(r/128, c/128)
+ *             weight (r, c) = code(r, c) * scale(r/128, c/128); a block with scale 0 adds exactly nothing,
+ *             whatever its codes, and the channels of x that meet it, hold
  *   x         [T][K] in x_dtype FT_DT_BF16 or FT_DT_F32, brought into the row form by the call; or,
  *             with FT_DT_FP8_ACT, the codes of its row form, x_scales that form's scales (NULL
  *             and unused otherwise)

@@ -29,6 +29,20 @@ __device__ __forceinline__ i32x8_vec_t codes32(const uint8_t *p) {
                        static_cast<int>(hi.x), static_cast<int>(hi.y), static_cast<int>(hi.z), static_cast<int>(hi.w)};
 }
 
+// 16 x 16 products over one block of 128, scaled by e8m0, added to z (WIDE: the arithmetic of float32 results)
+template <bool WIDE>
+__device__ __forceinline__ floatx4_t block_product(i32x8_vec_t a, int sa, i32x8_vec_t b, int sb, floatx4_t z) {
+    if constexpr (WIDE) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(act_bf16x8(a[2 * q], a[2 * q + 1], act_scale_operand(sa)),
+                                                        act_bf16x8(b[2 * q], b[2 * q + 1], act_scale_operand(sb)), z, 0, 0, 0);
+        return z;
+    } else {
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, z, 0, 0, 0, sa, 0, sb);
+    }
+}
+
 // four consecutive results: 0 bf16 (rounded once, to nearest even), 1 float32, 2 added to the float32 there
 template <int OUT>
 __device__ __forceinline__ void store4(void *out, size_t at, floatx4_t v) {
@@ -79,7 +93,6 @@ __global__ __launch_bounds__(256) void product_join(ProductArgs p, int parts) {
 // by every wave were no faster.
 template <int RA, int TB, int W, int ASC, int BX, bool WIDE, int OUT>
 __global__ __launch_bounds__(64 * W) void product_direct(ProductArgs p) {
-    constexpr bool kWide = WIDE;
     constexpr int kTile = RA * TB * 256;
     static_assert(BX == 0 || TB == 1, "quantised rows fit one operand");
     __shared__ float red[W / 2][kTile];
@@ -170,19 +183,11 @@ __global__ __launch_bounds__(64 * W) void product_direct(ProductArgs p) {
             else sa = static_cast<const uint8_t *>(p.as)[static_cast<size_t>(kb) * p.asr + min(a0 + 16 * i + r, p.M - 1)];
 #pragma unroll
             for (int j = 0; j < TB; ++j) {
-                floatx4_t z = ASC == 0 ? floatx4_t{} : acc[i][j];
-                if constexpr (kWide) {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                            act_bf16x8(a[i][2 * q], a[i][2 * q + 1], act_scale_operand(sa)),
-                            act_bf16x8(b[j][2 * q], b[j][2 * q + 1], act_scale_operand(sb[j])), z, 0, 0, 0);
-                } else {
-                    z = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a[i], b[j], z, 0, 0, 0, sa, 0, sb[j]);
-                }
+                const floatx4_t z = block_product<WIDE>(a[i], sa, b[j], sb[j], ASC == 0 ? floatx4_t{} : acc[i][j]);
+                // a weight block with scale 0 adds nothing, whatever its codes and the rows hold
                 if constexpr (ASC == 0)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) acc[i][j][q] = fmaf(sw, z[q], acc[i][j][q]);
+                    for (int q = 0; q < 4; ++q) acc[i][j][q] = fmaf(sw, sw == 0.0f ? 0.0f : z[q], acc[i][j][q]);
                 else acc[i][j] = z;
             }
         }
@@ -217,6 +222,27 @@ __global__ __launch_bounds__(64 * W) void product_direct(ProductArgs p) {
             if (a < p.M) store4<OUT>(split_out(p), static_cast<size_t>(b) * p.M + a, acc[i][j]);   // M is a multiple of 16
         }
     }
+}
+
+// One 16 x 16 tile at (a0, b0) by one wave from global memory, without the weight blocks of scale 0.
+template <bool WIDE, int OUT>
+__device__ __forceinline__ void again(const ProductArgs &p, int a0, int b0, int k0, int k1) {
+    const int lane = lane_id(), r = lane & 15, g = lane >> 4, nkb = p.Kp / 128;
+    if (a0 >= p.M) return;   // M is a multiple of 16
+    const int row = min(b0 + r, p.R - 1);
+    const uint8_t *pa = p.a + static_cast<size_t>(a0 + r) * p.Kp + 16 * g, *pb = p.b + static_cast<size_t>(row) * p.Kp + 16 * g;
+    const float *scale = static_cast<const float *>(p.as) + static_cast<size_t>(a0 / 128) * nkb;
+    floatx4_t acc{};
+#pragma unroll 1
+    for (int kb = k0; kb < k1; ++kb) {
+        const float f = scale[kb];
+        if (f == 0.0f) continue;
+        const size_t at = static_cast<size_t>(kb) * 128;
+        const floatx4_t z = block_product<WIDE>(codes32(pa + at), 127, codes32(pb + at), p.bs[kb * static_cast<size_t>(p.bsr) + row], floatx4_t{});
+#pragma unroll
+        for (int q = 0; q < 4; ++q) acc[q] = fmaf(f, z[q], acc[q]);
+    }
+    if (b0 + r < p.R) store4<OUT>(split_out(p), static_cast<size_t>(b0 + r) * p.M + a0 + 4 * g, acc);
 }
 
 // Tiled kernel: a workgroup of GA x GB waves owns a tile of 16 WA GA rows of A by 16 WB GB rows of B, each
@@ -345,6 +371,7 @@ __global__ __launch_bounds__(64 * GA * GB, 2) void product_tiled(ProductArgs p, 
         sb[j] = lbs[16 * j];
     }
     float sw = weight_scale(0), swz_old = 0.0f;   // weight scale of this block, and of the sums in z
+    uint32_t least = 1;                           // 0 once a weight scale was 0
     int s0 = 0;                                   // A slot of the block's first half
     auto after = [&](int slot) { return slot + kHalf == kAHalves * kHalf ? 0 : slot + kHalf; };
     // one block; `more`: there are blocks to request
@@ -454,6 +481,7 @@ __global__ __launch_bounds__(64 * GA * GB, 2) void product_tiled(ProductArgs p, 
             a = an;
             sa = san;
         });
+        if (!ASC) least = min(least, __float_as_uint(sw) << 1);
         swz_old = sw;
         sw = sw_next;
         s0 = s2;
@@ -472,6 +500,27 @@ __global__ __launch_bounds__(64 * GA * GB, 2) void product_tiled(ProductArgs p, 
     constexpr int kSize = OUT == 0 ? 2 : 4, kRow = 16 * WA * kSize, kPitch = kRow + 16, kLanes = kRow / 16;
     static_assert(16 * kPitch * NW <= sizeof(lds), "epilogue");
     stage_barrier();   // every wave has read its last operands, and its requests have landed
+    // A weight block with scale 0 adds nothing, whatever its codes and the rows that meet them hold.  Where those are
+    // finite its product was 0 already; where a sum is NaN the wave forms its sums again without such blocks, in the
+    // same order, straight from global memory.  (In the loop it would take a branch around a block, whose two sides
+    // spill, or an instruction more for every sum.)
+    if constexpr (!ASC) {
+        static_assert(128 % (16 * WA) == 0, "a wave's rows of A lie in one weight block");
+        bool nan = false;
+        if (__builtin_expect(__builtin_amdgcn_readfirstlane(least) == 0, 0))
+#pragma unroll
+            for (int i = 0; i < WA; ++i)
+#pragma unroll
+                for (int j = 0; j < WB; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) nan |= acc[i][j][q] != acc[i][j][q];
+        if (__builtin_expect(__ballot(nan) != 0, 0)) {
+#pragma unroll 1
+            for (int t = 0; t < WA * WB; ++t)
+                again<WIDE, OUT>(p, a0 + (wa * WA + t / WB) * 16, b0 + (wb * WB + t % WB) * 16, k0, k1);
+            return;
+        }
+    }
     uint8_t *mine = lds + wave * 16 * kPitch;
 #pragma unroll
     for (int j = 0; j < WB; ++j) {
