@@ -160,7 +160,10 @@ __global__ __launch_bounds__(kActThreads) void act_quantize(const XT *x, int T, 
     for (int r = 0; r < kActRows; ++r)
         load8(x + static_cast<size_t>(min(row0 + r, T - 1)) * C + min(c, C - 8), v[0][r]);
 #pragma unroll
-    for (int r = 0; r < kActRows; ++r) zero_unless(row0 + r < T && c < C, v[0][r]);   // C is a multiple of 16
+    for (int r = 0; r < kActRows; ++r) {
+        quiet(v[0][r]);
+        zero_unless(row0 + r < T && c < C, v[0][r]);   // C is a multiple of 16
+    }
     const ActPlane to[1] = {{row, cb, col, cb * 128}};
     put_tile<1>(v, sh, to, rb * 128, rb);
 }
@@ -180,6 +183,7 @@ __global__ __launch_bounds__(256) void act_quantize_rows(const XT *x, int T, int
     }
 #pragma unroll
     for (int r = 0; r < kRowsPerLane; ++r) {
+        quiet(v[r]);
         zero_unless(row0 + 32 * r < T && c < C, v[r]);   // C is a multiple of 16
         put_row(v[r], f, row0 + 32 * r, T, kb, sub);
     }
@@ -211,6 +215,8 @@ __global__ __launch_bounds__(256) void swiglu_quantize(const XT *gu, int T, int 
     float g[16], u[16], hv[16];
     load16(p, g);
     load16(p + I, u);
+    quiet(g);
+    quiet(u);
     zero_unless(row < T, g);
     zero_unless(row < T, u);
 #pragma unroll

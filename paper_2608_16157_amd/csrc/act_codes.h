@@ -83,8 +83,16 @@ __device__ __forceinline__ void load8(const float *p, float *v) {
     }
 }
 
+// Values as they come from memory, with signalling NaNs made quiet.  Results of arithmetic are quiet already.
+template <int N>
+__device__ __forceinline__ void quiet(float (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = __builtin_canonicalizef(v[i]);
+}
+
 // max(m, |a|, |b|) in one instruction.  The compiler takes four: it clears the signs and quiets the operands
-// first.  NaN operands drop out or make the result NaN; both are looked after where it is used.
+// first.  A quiet NaN drops out.  A signalling one would take the maximum so far with it (it makes that a quiet NaN,
+// which the next step drops), so values of memory go through quiet() before.
 __device__ __forceinline__ float max3_abs(float m, float a, float b) {
     float r;
     asm("v_max3_f32 %0, %1, |%2|, |%3|" : "=v"(r) : "v"(m), "v"(a), "v"(b));

@@ -145,6 +145,7 @@ __global__ __launch_bounds__(64 * W) void product_direct(ProductArgs p) {
             for (int q = 0; q < kOnWay; ++q) {
                 const int i = first + q * kLaneRows;
                 if (i >= n) break;
+                quiet(v[q]);
                 if (i % nkb * 128 + 8 * sub >= p.K)   // K is a multiple of 16
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[q][e] = 0.0f;

@@ -73,3 +73,64 @@ def test_linear_blocks_of_scale_0_meet_what_is_not_finite(T, N, K):
     for yd in (BF16, F32):
         want = run_linear(N, K, T, wt, x, BF16, yd)
         assert torch.isfinite(want).all() and torch.equal(run_linear(N, K, T, wt, bad, BF16, yd), want)
+
+
+# ----------------------------------------------------------------------------- signalling NaNs
+
+@pytest.mark.parametrize("dtype", (BF16, F32))
+@pytest.mark.parametrize("T,C", ((40, 256), (130, 400), (257, 128)))
+def test_signalling_nans_leave_their_block_its_scale(T, C, dtype):
+    """Signalling NaNs anywhere in a block, in front of, behind and between values of many magnitudes: NaN codes, and
+    the scale and the other codes those of the block without them."""
+    r = rng(T, C, dtype, 32)
+    x = (r.normal(size=(T, C)) * 10.0 ** r.uniform(-3, 3, (T, C))).astype(np.float32)
+    if dtype == BF16:
+        bits = (x.view(np.uint32) >> 16).astype(np.uint16)
+        snan, quiet = np.uint16([0x7F81, 0xFFBF]), np.uint16([0x7FC0, 0xFFC1])
+    else:
+        bits = x.view(np.uint32).copy()
+        snan, quiet = np.uint32([0x7F800001, 0xFFBFFFFF]), np.uint32([0x7FC00000, 0xFFC00001])
+    at = r.random((T, C)) < 0.1
+    bits[at] = r.choice(snan, size=int(at.sum()))
+    bits[0, :128] = snan[0]
+    bits[1, :127] = snan[1]   # one value of its block left
+    some = r.random((T, C)) < 0.02
+    bits[some] = r.choice(quiet, size=int(some.sum()))
+    x = (bits.astype(np.uint32) << 16 if dtype == BF16 else bits).view(np.float32)
+    t = torch.from_numpy(bits.view(np.int16 if dtype == BF16 else np.int32)).cuda().view(TORCH[dtype])
+
+    def check(c, v):
+        with np.errstate(invalid="ignore"):
+            codes, s = dense.quantize(v.astype(np.float64))
+        got = c.codes.cpu().numpy()
+        nan = (codes & 0x7F) == 0x7F
+        assert np.array_equal(c.scales.cpu().numpy()[:, :v.shape[0]], s)
+        assert np.array_equal((got & 0x7F) == 0x7F, nan) and np.array_equal(got[~nan], codes[~nan])
+
+    row, col, alone = filled(T, C), filled(C, T), filled(T, C)
+    ftm.ft_act_quantize(t, T, C, row, col)
+    ftm.ft_act_quantize(t, T, C, alone)
+    check(alone, x)
+    check(row, x)
+    check(col, x.T)
+    if C % 256 == 0:   # kept by SwiGLU
+        h, saved = filled(T, C // 2), filled(T, C)
+        ftm.ft_swiglu_quantize(t, T, C // 2, h, saved)
+        check(saved, x)
+
+
+def test_signalling_nans_inside_the_product():
+    """Rows that the product quantises itself: the other rows are not touched, and a row's NaNs that meet only weight
+    blocks of scale 0 leave the row's other blocks as they are."""
+    T, N, K = 4, 64, 512
+    r = rng(33)
+    wt, w = weight(r, N, K)
+    xv, x = matrix(r, T, K, BF16, spread=1)
+    x.view(torch.int16)[1, 200] = 0x7F81
+    x.view(torch.int16)[1, 130] = -1          # a quiet one
+    y = run_linear(N, K, T, wt, x, BF16, F32)
+    q = form_of(np.where(np.isfinite(f64(x)), f64(x), 0.0))[1]
+    keep = [0, 2, 3]
+    assert_product(y[keep], q[keep] @ w.T, np.abs(q[keep]) @ np.abs(w).T, K, F32)
+    wt["s"][:, 1], w[:, 128:256] = 0, 0
+    assert_product(run_linear(N, K, T, wt, x, BF16, F32), q @ w.T, np.abs(q) @ np.abs(w).T, K, F32)
