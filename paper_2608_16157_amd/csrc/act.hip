@@ -274,7 +274,7 @@ __global__ __launch_bounds__(kActThreads, 4) void swiglu_backward(ActForm saved,
             const float gs = g[q] * s;
             v[2][r][q] = gs * u[q];
             v[1][r][q] = d[r][q] * gs;
-            v[0][r][q] = d[r][q] * u[q] * (s + gs * (1.0f - s));
+            v[0][r][q] = d[r][q] * (u[q] * (s + gs * (1.0f - s)));   // dh u alone may overflow
         }
 #pragma unroll
         for (int n = 0; n < 3; ++n) zero_unless(row0 + r < T, v[n][r]);

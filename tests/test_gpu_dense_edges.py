@@ -134,3 +134,29 @@ def test_signalling_nans_inside_the_product():
     assert_product(y[keep], q[keep] @ w.T, np.abs(q[keep]) @ np.abs(w).T, K, F32)
     wt["s"][:, 1], w[:, 128:256] = 0, 0
     assert_product(run_linear(N, K, T, wt, x, BF16, F32), q @ w.T, np.abs(q) @ np.abs(w).T, K, F32)
+
+
+# ------------------------------------------------------------------------------ SwiGLU backward
+
+@pytest.mark.parametrize("gate", (-60.0, -144.0))
+def test_swiglu_gradient_whose_factors_overflow(gate):
+    """dh up past float32's largest value where the sigmoid brings the gradient back: d_gate is finite, and no NaN code
+    is left.  At gate -60 every element of a block is such a product; at -144, where the sigmoid is 0 in float32, one in
+    a block of ordinary ones."""
+    T, I = 3, 128
+    gv, dv = np.ones((T, 2 * I)), np.full((T, I), 2.0 ** -100)
+    gv[:, I:] = 2.0 ** 100
+    cols = slice(0, I) if gate == -60.0 else slice(5, 6)
+    gv[:, cols], dv[:, cols] = gate, 2.0 ** 40
+    saved, kept = form_of(gv)
+    assert np.array_equal(kept, gv)
+    want = dense.swiglu_grad(gv, dv)
+    assert np.isfinite(want).all() and np.abs(want).max() < 1e37
+    for dtype in (BF16, F32):
+        row, col = filled(T, 2 * I), filled(2 * I, T)
+        ftm.ft_swiglu_backward(saved, cuda(dv).to(TORCH[dtype]), T, I, row, col)
+        assert_near_form(row, want)
+        codes = col.codes.cpu().numpy()
+        assert not ((codes & 0x7F) == 0x7F).any()
+        if gate == -60.0:
+            assert_near_form(col, want.T)
