@@ -14,8 +14,10 @@
 // no step across rows and serve four tokens at once, above by the whole wave (256 experts in a row take 138
 // registers: backward 49.8 us against 48.5 for 65536 tokens).  The next token is requested before the current
 // one is worked on: 65536 tokens of 256 experts backward 34.7 us, 4.1 TB/s (a copy of as much 25.5; the vector unit
-// works half of the time).  The sums over tokens stay in the lanes' registers.  Every sum is in float32 in a
-// fixed order: the results are the same in every run.
+// works half of the time).  The sums over tokens stay in the lanes' registers.  Every sum runs in a fixed order: the
+// results are the same in every run.  Sums over tokens are in float64 and rounded to float32 once for each wave
+// and once for each part, so that their error does not grow with the tokens: of equal probabilities, whose roundings
+// all point one way, float32 sums were off by 2e-6 for 20011 tokens.
 //
 // Forward: up to 512 tokens one launch, a workgroup per sequence (48 tokens of 128 experts 4.5 us); above, parts of the
 // tokens over up to 256 workgroups and a join (8192 tokens of 256 experts in 9 sequences 12.6 us: two launches,
@@ -53,6 +55,27 @@ __device__ __forceinline__ float lanes_sum(float v) {
     v += ror(v, std::integral_constant<int, kDppRowRor4>{});
     v += ror(v, std::integral_constant<int, kDppRowRor8>{});
     return v;
+}
+
+// The same in float64 over the 16 lanes of a row, and over the lanes of the four rows that are one above the other.
+__device__ __forceinline__ double row_sum_f64(double v) {
+    auto ror = [](double x, auto c) {
+        constexpr int C = decltype(c)::value;
+        return __hiloint2double(static_cast<int>(dpp_u32<C>(__double2hiint(x))), static_cast<int>(dpp_u32<C>(__double2loint(x))));
+    };
+    v += ror(v, std::integral_constant<int, kDppRowRor1>{});
+    v += ror(v, std::integral_constant<int, kDppRowRor2>{});
+    v += ror(v, std::integral_constant<int, kDppRowRor4>{});
+    v += ror(v, std::integral_constant<int, kDppRowRor8>{});
+    return v;
+}
+__device__ __forceinline__ double rows_sum_f64(double v) {
+    uint32_t lo = __double2loint(v), hi = __double2hiint(v);
+    const auto l16 = __builtin_amdgcn_permlane16_swap(lo, lo, false, false), h16 = __builtin_amdgcn_permlane16_swap(hi, hi, false, false);
+    v = __hiloint2double(h16[0], l16[0]) + __hiloint2double(h16[1], l16[1]);
+    lo = __double2loint(v), hi = __double2hiint(v);
+    const auto l32 = __builtin_amdgcn_permlane32_swap(lo, lo, false, false), h32 = __builtin_amdgcn_permlane32_swap(hi, hi, false, false);
+    return __hiloint2double(h32[0], l32[0]) + __hiloint2double(h32[1], l32[1]);
 }
 
 // How a token's E values lie in its LPT lanes, NE each: four consecutive ones at a time where every row is
@@ -103,8 +126,8 @@ __device__ __forceinline__ void sigmoid_parts(float x, float &e, float &r) {
 // mode a = 1 - sigmoid(l).  The sigmoids of a token whose logits are all negative are taken relative to exp
 // of the largest, exp(l - c) / (1 + exp(l)), so that they do not all vanish in float32.  A token whose
 // logits are all -inf has no probabilities: p = 0.
-template <class L>
-__device__ __forceinline__ void router_probs(const float (&l)[L::NE], int gating, float (&p)[L::NE], float (&a)[L::NE]) {
+template <class L, bool kA>   // kA: a is asked for (its registers otherwise hold the sums over the tokens)
+__device__ __forceinline__ void router_probs(const float (&l)[L::NE], int gating, float (&p)[L::NE], float (&a)[kA ? L::NE : 1]) {
     float m = l[0];
 #pragma unroll
     for (int i = 1; i < L::NE; ++i) m = fmaxf(m, l[i]);
@@ -114,7 +137,7 @@ __device__ __forceinline__ void router_probs(const float (&l)[L::NE], int gating
 #pragma unroll
         for (int i = 0; i < L::NE; ++i) {
             p[i] = __expf(l[i] - m);
-            a[i] = 1.0f;
+            if constexpr (kA) a[i] = 1.0f;
             sum += p[i];
         }
     } else {
@@ -123,14 +146,19 @@ __device__ __forceinline__ void router_probs(const float (&l)[L::NE], int gating
             float e, r;
             sigmoid_parts(l[i], e, r);
             p[i] = l[i] > 0.0f ? r : e * r;
-            a[i] = l[i] > 0.0f ? e * r : r;
+            if constexpr (kA) a[i] = l[i] > 0.0f ? e * r : r;
         }
         // a positive logit anywhere in the wave is the common case; without one the maximum is looked for
         if (L::LPT != 64 || !__any(m > 0.0f)) {
             m = lanes_max<L::LPT>(m);
             if (m < 0.0f)
 #pragma unroll
-                for (int i = 0; i < L::NE; ++i) p[i] = __expf(l[i] - m) * a[i];
+                for (int i = 0; i < L::NE; ++i) {
+                    float e, r;
+                    if constexpr (kA) r = a[i];
+                    else sigmoid_parts(l[i], e, r);
+                    p[i] = __expf(l[i] - m) * r;
+                }
         } else {
             m = 1.0f;   // not -inf
         }
@@ -194,13 +222,13 @@ struct BalanceShared {
 // Sums of the tokens [beg, end) over the workgroup: thread e < E gets its expert's probability sum and
 // count, every thread the number of counted tokens.
 template <class L>
-__device__ __forceinline__ void sum_tokens(const BalanceArgs &b, BalanceShared<L> &sh, int beg, int end, float &prob,
+__device__ __forceinline__ void sum_tokens(const BalanceArgs &b, BalanceShared<L> &sh, int beg, int end, double &prob,
                                            int &count, int &tokens) {
     constexpr int kE = BalanceShared<L>::kE;
     const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t / 64), lane = lane_id(), sub = lane % L::LPT;
-    float acc[L::NE];
+    double acc[L::NE];
 #pragma unroll
-    for (int i = 0; i < L::NE; ++i) acc[i] = 0.0f;
+    for (int i = 0; i < L::NE; ++i) acc[i] = 0.0;
     // the next token's logits and ids are requested before the current one is worked on
     constexpr int kStep = kBalWaves * L::kTokens;
     int n = 0, tok = beg + wave * L::kTokens + lane / L::LPT;
@@ -218,7 +246,7 @@ __device__ __forceinline__ void sum_tokens(const BalanceArgs &b, BalanceShared<L
     if (t == 0) sh.tokens = 0;
     __syncthreads();
     for (; tok < end; tok += kStep) {
-        float l[L::NE], p[L::NE], a[L::NE];
+        float l[L::NE], p[L::NE], a[1];
 #pragma unroll
         for (int i = 0; i < L::NE; ++i) l[i] = next[i];
         int id = id_next;
@@ -229,7 +257,7 @@ __device__ __forceinline__ void sum_tokens(const BalanceArgs &b, BalanceShared<L
             if (j != sub) id = b.topk_ids[static_cast<size_t>(tok) * b.k + j];
             if (id >= 0 && id < b.E) atomicAdd(&sh.count[id], 1);
         }
-        router_probs<L>(l, b.gating, p, a);
+        router_probs<L, false>(l, b.gating, p, a);
 #pragma unroll
         for (int i = 0; i < L::NE; ++i) acc[i] += p[i];
         ++n;
@@ -237,44 +265,43 @@ __device__ __forceinline__ void sum_tokens(const BalanceArgs &b, BalanceShared<L
     if (sub == 0 && n) atomicAdd(&sh.tokens, n);
 #pragma unroll
     for (int i = 0; i < L::NE; ++i) {
-        if constexpr (L::LPT == 16) {   // the wave's four tokens
-            acc[i] += __shfl_xor(acc[i], 16);
-            acc[i] += __shfl_xor(acc[i], 32);
-        }
-        if (lane < L::LPT) sh.prob[wave][L::expert(sub, i)] = acc[i];
+        if constexpr (L::LPT == 16) acc[i] = rows_sum_f64(acc[i]);   // the wave's four tokens
+        if (lane < L::LPT) sh.prob[wave][L::expert(sub, i)] = static_cast<float>(acc[i]);
     }
     __syncthreads();
-    prob = 0.0f;
+    prob = 0.0;
     count = 0;
     tokens = sh.tokens;
     if (t < kE) {
+        double part[4] = {};   // four sums at once: their additions wait for one another
 #pragma unroll
-        for (int w = 0; w < kBalWaves; ++w) prob += sh.prob[w][t];
+        for (int w = 0; w < kBalWaves; ++w) part[w % 4] += sh.prob[w][t];
+        prob = (part[0] + part[1]) + (part[2] + part[3]);
         count = sh.count[t];
     }
     __syncthreads();
 }
 
 // Outputs of sequence s from its sums (thread e holds expert e's).
-__device__ __forceinline__ void finish_seq(const BalanceArgs &b, int s, float prob, int count, int tokens, float *red) {
+__device__ __forceinline__ void finish_seq(const BalanceArgs &b, int s, double prob, int count, int tokens, double *red) {
     const int t = threadIdx.x;
-    float term = 0.0f;
+    double term = 0.0;
     if (t < b.E) {
-        const float n = static_cast<float>(max(tokens, 1));
-        const float P = prob / n, f = b.coef * static_cast<float>(b.E) * static_cast<float>(count) / (static_cast<float>(b.k) * n);
+        const double inv = 1.0 / max(tokens, 1), P = prob * inv, f = b.frac_scale * count * inv;
         const size_t o = static_cast<size_t>(s) * b.E + t;
         b.counts[o] = count;
-        b.prob[o] = P;
-        b.frac[o] = f;
+        b.prob[o] = static_cast<float>(P);
+        b.frac[o] = static_cast<float>(f);
         term = f * P;
     }
-    const float ws = wave_sum_f32(term);
-    if (lane_id() == 0) red[t / 64] = ws;
+    term = rows_sum_f64(row_sum_f64(term));
+    if (lane_id() == 0) red[t / 64] = term;
     __syncthreads();
+    if (t >= 16) return;
+    static_assert(kBalWaves == 16, "a row of lanes");
+    const double loss = row_sum_f64(red[t]);
     if (t == 0) {
-        float L = 0.0f;
-        for (int w = 0; w < kBalWaves; ++w) L += red[w];
-        b.loss[s] = L;
+        b.loss[s] = static_cast<float>(loss);
         b.tokens[s] = tokens;
     }
 }
@@ -283,10 +310,10 @@ __device__ __forceinline__ void finish_seq(const BalanceArgs &b, int s, float pr
 template <class L>
 __global__ __launch_bounds__(kBalThreads) void balance_whole(BalanceArgs b) {
     __shared__ BalanceShared<L> sh;
-    __shared__ float red[kBalWaves];
+    __shared__ double red[kBalWaves];
     const int s = blockIdx.x;
     int beg, end, count, tokens;
-    float prob;
+    double prob;
     seq_bounds(b, s, beg, end);
     sum_tokens<L>(b, sh, beg, end, prob, count, tokens);
     finish_seq(b, s, prob, count, tokens, red);
@@ -301,7 +328,7 @@ __global__ __launch_bounds__(kBalThreads) void balance_parts(BalanceArgs b) {
     const WaveSeqs seqs(b);
     for (int s = seqs.first_after(p0); s < b.n_seq; ++s) {
         int beg, end, count, tokens;
-        float prob;
+        double prob;
         seqs.bounds(s, beg, end);
         if (beg >= p1) break;
         beg = max(beg, p0);
@@ -310,7 +337,7 @@ __global__ __launch_bounds__(kBalThreads) void balance_parts(BalanceArgs b) {
         sum_tokens<L>(b, sh, beg, end, prob, count, tokens);
         const size_t row = static_cast<size_t>(q) + s;
         if (threadIdx.x < b.E) {
-            b.ws_sums[row * b.E + threadIdx.x] = float2{prob, __int_as_float(count)};
+            b.ws_sums[row * b.E + threadIdx.x] = float2{static_cast<float>(prob), __int_as_float(count)};
         }
         if (threadIdx.x == 0) b.ws_tokens[row] = tokens;
     }
@@ -321,16 +348,16 @@ __global__ __launch_bounds__(kBalThreads) void balance_parts(BalanceArgs b) {
 template <int EP>
 __global__ __launch_bounds__(kBalThreads) void balance_join(BalanceArgs b) {
     constexpr int kSide = kBalThreads / EP;
-    __shared__ float s_prob[kSide][EP];
+    __shared__ double s_prob[kSide][EP];
     __shared__ int32_t s_count[kSide][EP];
     __shared__ int32_t s_tokens;
-    __shared__ float red[kBalWaves];
+    __shared__ double red[kBalWaves];
     const int s = blockIdx.x, t = threadIdx.x, e = t % EP, side = t / EP;
     int beg, end;
     seq_bounds(b, s, beg, end);
     if (t == 0) s_tokens = 0;
     __syncthreads();
-    float prob = 0.0f;
+    double prob = 0.0;
     int count = 0;
     if (beg < end) {
         const int q0 = beg / b.part_tokens, q1 = (end - 1) / b.part_tokens;
@@ -341,14 +368,16 @@ __global__ __launch_bounds__(kBalThreads) void balance_join(BalanceArgs b) {
         if (e < b.E)
             for (int q = q0 + side; q <= q1; q += kAhead * kSide) {
                 float2 v[kAhead];
+                double part[4] = {};
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i) v[i] = b.ws_sums[(static_cast<size_t>(min(q + i * kSide, q1)) + s) * b.E + e];
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i)
                     if (q + i * kSide <= q1) {
-                        prob += v[i].x;
+                        part[i % 4] += v[i].x;
                         count += __float_as_int(v[i].y);
                     }
+                prob += (part[0] + part[1]) + (part[2] + part[3]);
             }
         if (q0 + t <= q1 && n) atomicAdd(&s_tokens, n);
     }
@@ -427,7 +456,7 @@ __global__ __launch_bounds__(256) void router_grad(BalanceArgs b, int run) {
             L::load(b.frac + static_cast<size_t>(s) * b.E, b.E, sub, 0.0f, f);
         }
         float p[L::NE], a[L::NE], d[L::NE];
-        router_probs<L>(cur.l, b.gating, p, a);
+        router_probs<L, true>(cur.l, b.gating, p, a);
         if (b.d_topk_w) {
             float dot = 0.0f;
 #pragma unroll

@@ -91,7 +91,7 @@ BalanceArgs balance_args(const ft_balance_desc_t *d, const float *logits, const 
     a.k = d->top_k;
     a.gating = d->gating;
     a.n_seq = d->n_seq;
-    a.coef = d->coef;
+    a.frac_scale = static_cast<double>(d->coef) * d->n_experts / d->top_k;
     if (b) {
         a.counts = b->counts;
         a.tokens = b->tokens;

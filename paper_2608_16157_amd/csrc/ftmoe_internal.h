@@ -67,7 +67,7 @@ struct BalanceArgs {
     const int32_t *seq_off;    // [n_seq + 1] or null (one sequence of T)
     const uint8_t *mask;       // [T] or null
     int T, E, k, gating, n_seq;
-    float coef;
+    double frac_scale;         // coef E / k
     int32_t *counts;           // [n_seq][E]
     int32_t *tokens;           // [n_seq]
     float *prob, *frac;        // [n_seq][E]

@@ -160,3 +160,22 @@ def test_swiglu_gradient_whose_factors_overflow(gate):
         assert not ((codes & 0x7F) == 0x7F).any()
         if gate == -60.0:
             assert_near_form(col, want.T)
+
+
+# ---------------------------------------------------------------------------------- long sums
+
+@pytest.mark.parametrize("T,E", ((511, 7), (8191, 300), (20011, 300), (100003, 131), (100003, 1000), (1000003, 11)))
+def test_balance_sums_do_not_drift(T, E):
+    """Equal logits: every probability is the same float32, the rounded 1 / E, and its sum over the tokens must stay
+    exact but for roundings that do not grow with the tokens: one of each wave's sum, one of each part's and one of
+    the result, 2^-24 of it each as all terms are positive.  (A float32 running sum of equal terms is off by tens of
+    such steps.)  frac is exact to its rounding, and the loss has one more rounding."""
+    desc = {"n_experts": E, "top_k": 1, "gating": 0, "n_seq": 1, "coef": 1.0}
+    ids = torch.zeros(T, 1, dtype=torch.int32, device="cuda")
+    out = ftm.BalanceBuffers(1, E)
+    ftm.ft_balance_loss(desc, torch.zeros(T, E, device="cuda"), ids, T, out, ftm.alloc_balance_workspace(desc, T))
+    p = float(np.float32(1) / np.float32(E))
+    assert np.all(np.abs(f64(out.prob) - p) <= 3 * 2.0 ** -24 * p)
+    assert np.array_equal(f64(out.frac)[0], [E] + [0] * (E - 1))
+    assert abs(f64(out.loss)[0] - p * E) <= 4 * 2.0 ** -24 * p * E
+    assert out.tokens.item() == T and out.counts[0, 0].item() == T
