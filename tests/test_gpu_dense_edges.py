@@ -179,3 +179,68 @@ def test_balance_sums_do_not_drift(T, E):
     assert np.array_equal(f64(out.frac)[0], [E] + [0] * (E - 1))
     assert abs(f64(out.loss)[0] - p * E) <= 4 * 2.0 ** -24 * p * E
     assert out.tokens.item() == T and out.counts[0, 0].item() == T
+
+
+# ------------------------------------------------------------------------- branches of the router
+
+def router_both_ways(desc, logits, ids, off, mask, r):
+    """Forward and backward against the oracle, with the bounds of the module these helpers come from."""
+    T, E, k, n_seq, gating = *logits.shape, desc["top_k"], desc["n_seq"], desc["gating"]
+    out = ftm.BalanceBuffers(n_seq, E)
+    args = dict(seq_off=cuda(off), mask=None if mask is None else cuda(mask))
+    ftm.ft_balance_loss(desc, cuda(logits), cuda(ids), T, out, ftm.alloc_balance_workspace(desc, T), **args)
+    l64 = logits.astype(np.float64)
+    want = dense.balance(l64, ids, off, mask, gating, desc["coef"])
+    assert np.array_equal(out.counts.cpu().numpy(), want["counts"])
+    assert np.array_equal(out.tokens.cpu().numpy(), want["tokens"])
+    for n in ("prob", "frac", "loss"):
+        assert np.all(np.abs(f64(getattr(out, n)) - want[n]) <= 2e-5 * np.abs(want[n]) + 1e-30), n
+    sel = np.take_along_axis(l64, np.clip(ids, 0, E - 1), 1)
+    v = np.exp(sel - sel.max(1, keepdims=True)) if gating == oracle.GATE_SOFTMAX else dense.sigmoid(sel)
+    gates = (v / v.sum(1, keepdims=True)).astype(np.float32)
+    dw, dl = r.normal(size=(T, k)).astype(np.float32), r.normal(size=n_seq).astype(np.float32)
+    d = torch.full((T, E), 13.0, device="cuda")
+    ftm.ft_router_backward(desc, cuda(logits), cuda(ids), T, out, cuda(dl), d, topk_w=cuda(gates), d_topk_w=cuda(dw), **args)
+    g, mag = dense.router_grad(l64, ids, gates.astype(np.float64), dw.astype(np.float64), off, mask, gating, f64(out.frac),
+                               dl.astype(np.float64))
+    got, outside = f64(d), np.isnan(g)
+    assert outside.any() == (off[0] > 0 or off[-1] < T) and np.all(got[outside] == 13.0)
+    assert np.all(np.abs(got - g)[~outside] <= 2e-5 * mag[~outside] + 1e-30)
+
+
+def router_inputs(r, T, E, k):
+    logits = (r.normal(size=(T, E)) * 2).astype(np.float32)
+    return logits, np.argsort(-logits, axis=1, kind="stable")[:, :k].astype(np.int32)
+
+
+@pytest.mark.parametrize("gating", (oracle.GATE_SOFTMAX, oracle.GATE_SIGMOID))
+@pytest.mark.parametrize("T,E,k,n_seq", ((16385, 48, 5, 300), (20003, 128, 17, 40), (16387, 256, 8, 300), (17001, 320, 33, 64),
+                                         (16384, 64, 2, 1)))
+def test_router_of_many_tokens_and_short_sequences(T, E, k, n_seq, gating):
+    """Runs of four tokens a lane row: sequences of none to three tokens, so that several end inside a run, long ones
+    around them, tokens of none at both ends, a last run that is not whole."""
+    r = rng(T, E, gating, 34)
+    if n_seq > 1:
+        short = r.integers(0, 4, n_seq - 3)
+        first, middle = 1021, T // 2 + 1     # no multiples of a run
+        off = np.concatenate([[first, middle], middle + np.cumsum(short), [T - 1500, T - 7]]).astype(np.int32)
+    else:
+        off = np.array([0, T], np.int32)
+    assert len(off) == n_seq + 1 and np.all(np.diff(off) >= 0)
+    mask = (r.random(T) < 0.8).astype(np.uint8)
+    logits, ids = router_inputs(r, T, E, k)
+    router_both_ways({"n_experts": E, "top_k": k, "gating": gating, "n_seq": n_seq, "coef": 0.3}, logits, ids, off, mask, r)
+
+
+@pytest.mark.parametrize("gating", (oracle.GATE_SOFTMAX, oracle.GATE_SIGMOID))
+@pytest.mark.parametrize("E,k", ((64, 17), (64, 33), (64, 64), (128, 17), (128, 48), (100, 64)))
+@pytest.mark.parametrize("T", (1, 130, 700))
+def test_router_of_more_experts_a_token_than_lanes(T, E, k, gating):
+    """Up to 128 experts a token has 16 lanes: with more selected ones each lane holds several."""
+    r = rng(T, E, k, gating, 35)
+    off = np.array([0, T // 3, T], np.int32)
+    logits, ids = router_inputs(r, T, E, k)
+    if T > 1:
+        ids[::7, k - 1], ids[1::7, 16] = -1, E     # not counted
+    router_both_ways({"n_experts": E, "top_k": k, "gating": gating, "n_seq": 2, "coef": 0.3}, logits, np.ascontiguousarray(ids),
+                     off, None, r)
