@@ -244,3 +244,41 @@ def test_router_of_more_experts_a_token_than_lanes(T, E, k, gating):
         ids[::7, k - 1], ids[1::7, 16] = -1, E     # not counted
     router_both_ways({"n_experts": E, "top_k": k, "gating": gating, "n_seq": 2, "coef": 0.3}, logits, np.ascontiguousarray(ids),
                      off, None, r)
+
+
+# ------------------------------------------------------------------ the 256 x 256 tile, dense data
+
+@pytest.mark.parametrize("T,N,K", ((1922, 4256, 800), (2500, 4112, 1808)))
+def test_linear_of_the_largest_tile(T, N, K):
+    """7 and 15 blocks of reduction, so that every place of the tile's rings is filled more than once; rows, features
+    and the last block end inside a tile."""
+    r = rng(T, N, K, 36)
+    wt, w = weight(r, N, K)
+    xv, x = matrix(r, T, K, BF16, spread=1)
+    form, q = form_of(xv)
+    y = run_linear(N, K, T, wt, x, BF16, BF16)
+    assert_product(y, q @ w.T, np.abs(q) @ np.abs(w).T, K, BF16)
+    assert torch.equal(y, run_linear(N, K, T, wt, form, ACT, BF16))
+
+
+@pytest.mark.parametrize("T,N,K", ((803, 6800, 1168), (1000, 4096, 4096), (2004, 4752, 1936)))
+def test_weight_grad_of_the_largest_tile(T, N, K):
+    r = rng(T, N, K, 37)
+    dyv, xv = matrix(r, T, N, BF16, spread=1)[0], matrix(r, T, K, BF16, spread=1)[0]
+    (dc, a), (xc, b) = form_of(dyv.T), form_of(xv.T)
+    dw = torch.full((N + 1, K), 3.0, dtype=torch.bfloat16, device="cuda")
+    ftm.ft_linear_weight_grad(N, K, T, dc, xc, dw)
+    assert torch.all(dw[N] == 3.0)
+    assert_product(dw[:N], a @ b.T, np.abs(a) @ np.abs(b).T, T, BF16)
+
+
+def test_linear_of_the_largest_tile_split():
+    """A reduction long enough that even this tile's is split: 129 blocks in 7 parts."""
+    T, N, K = 132, 8272, 16496
+    r = rng(38)
+    wt, w = weight(r, N, K)
+    xv, x = matrix(r, T, K, BF16, spread=1)
+    form, q = form_of(xv)
+    y = run_linear(N, K, T, wt, form, ACT, BF16)
+    assert_product(y, q @ w.T, np.abs(q) @ np.abs(w).T, K, BF16)
+    assert torch.equal(y, run_linear(N, K, T, wt, form, ACT, BF16))
