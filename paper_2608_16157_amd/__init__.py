@@ -712,9 +712,6 @@ class ActCodes:
         self.rows, self.cols, self.codes, self.scales = rows, cols, codes, scales
         return self
 
-    def c(self) -> ft_act_codes_t:
-        return ft_act_codes_t(_ptr(self.codes), _ptr(self.scales))
-
 
 def _arg(dev: int, t, name: str, dtypes: tuple, numel: int):
     """The checks of _need, contiguity and one device for the whole call (``dev``: the one so far, -1 before the
@@ -918,9 +915,6 @@ class BalanceBuffers:
         self = cls.__new__(cls)
         self.counts, self.tokens, self.prob, self.frac, self.loss = counts, tokens, prob, frac, loss
         return self
-
-    def c(self) -> ft_balance_t:
-        return ft_balance_t(*[_ptr(getattr(self, n)) for n, _ in ft_balance_t._fields_])
 
 
 @functools.lru_cache(maxsize=256)
