@@ -550,7 +550,9 @@ ft_status_t ft_linear_transpose(int32_t out_features, int32_t in_features, const
                                 uint8_t *wt, float *wt_scales, void *stream);
 
 /*
- * Gradient of the weight, dw[N][K] = dy[T][N]^T x[T][K], from the column forms of dy and x.
+ * Gradient of the weight, dw[N][K] = dy[T][N]^T x[T][K], from the column forms of dy and x.  The reduction over the
+ * tokens is not split: a small weight runs on few compute units however long the batch is (8192 tokens of
+ * 576 x 512 20 us, of 7168 x 2048 99 us).
  *   dw_dtype   FT_DT_F32 or FT_DT_BF16, with the arithmetic of ft_linear's y_dtype
  *   accumulate 1: added to dw (float32 only, FT_ERR_DTYPE otherwise), 0: dw overwritten
  * T == 0 writes zeros (accumulate: leaves dw as it is).

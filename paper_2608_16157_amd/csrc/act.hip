@@ -5,14 +5,16 @@
 // All of these move memory once and compute little: the bound is HBM.
 //
 // The row form alone: 8 lanes per row and block of 128, 16 values a lane, so a block's maximum needs only
-// rotations within a lane row and no LDS.  8192 x 7168 bf16: 29 us, 6.05 TB/s.
+// rotations within a lane row and no LDS.  8192 x 7168 bf16: 29.7 us, 5.9 TB/s; float32 51 us,
+// 5.8 TB/s.
 //
 // The column form needs a maximum over 128 rows and the transposed codes: a workgroup owns a tile of
 // 128 x 128 elements, each thread a patch of 4 rows x 8 columns, so that the codes of 4 rows of a column
 // leave as one word through LDS and both forms store whole 128-byte lines.  Both forms of 8192 x 7168:
-// 40 us, 5.9 TB/s.  SwiGLU backward, three such planes at 9 bytes a channel: 8192 x 2048 in 38 us, 4.0 TB/s; the
-// vector unit works 0.4 of that, and with two tiles a CU (128 registers a thread) its work and the loads
-// overlap only between those two.  A tile after the other by the same workgroup, the next one's loads on the
+// 39 us, 6.0 TB/s (float32 69 us, 5.1 TB/s).  SwiGLU backward, three such planes at 9 bytes a channel: 8192 x 2048 in
+// 37 us, 4.1 TB/s; the vector unit works 0.45 of that, and with two tiles a CU (128 registers a thread, 76 KB of LDS a
+// tile) its work and the loads overlap only between those two; the columns' scales are read from LDS one by one,
+// each behind the write of the last one's codes.  A tile after the other by the same workgroup, the next one's loads on the
 // way, spills registers and is slower.
 #include "act_codes.h"
 #include "ftmoe_internal.h"
@@ -206,7 +208,7 @@ hipError_t launch_act_quantize(const void *x, bool f32, int T, int C, const ActF
 }
 
 // SwiGLU forward: h = silu(g) u from gu [T][2 I] (gate columns first), h in the row form and, if asked for,
-// gu itself.  8 lanes per (matrix row, block of 128 channels of h).  Bound: HBM; 8192 x 2048 in 20 us, 5.8 TB/s.
+// gu itself.  8 lanes per (matrix row, block of 128 channels of h).  Bound: HBM; 8192 x 2048 in 20.3 us, 5.8 TB/s.
 template <class XT>
 __global__ __launch_bounds__(256) void swiglu_quantize(const XT *gu, int T, int I, ActForm h, ActForm saved) {
     const int sub = threadIdx.x % 8, kb = blockIdx.x, nkb = I / 128;

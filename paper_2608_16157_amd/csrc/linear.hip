@@ -89,13 +89,14 @@ __global__ __launch_bounds__(256) void product_join(ProductArgs p, int parts) {
 
 // Direct kernel: operands from global memory to registers, the reduction split over the waves of a
 // workgroup and joined in LDS in a fixed order.  A wave holds 16 RA rows of A and 16 TB rows of B; lane
-// (r = lane % 16, g = lane / 16) the 32 codes [32 g, 32 g + 32) of row r of a block.
+// (r = lane % 16, g = lane / 16) 32 codes of row r of a block, [16 g, 16 g + 16) and the same 64 further on.
 // BX: 0 B is codes; 1 B is bf16, 2 float32: then every workgroup first brings the few rows into 8 bits in LDS
 // (the same in all of them: cheaper than a launch for up to kDirectTokens rows, kDirectBytes of codes).  ASC: 0 float32 block scales, 1 e8m0.
 // WIDE: the arithmetic of float32 results.  OUT: see store4.
 // Bound: one read of the weight, and at these times the launch and the chain of load, product and join:
 // 1 x 4096 x 7168 with its quantiser 7.7 us, 3.8 TB/s; 32 x 7168 x 2048 7.2 us.  Two more blocks requested ahead
-// by every wave were no faster.
+// by every wave were no faster, in a loop that waits on memory in other places too: as compiled, the second B
+// operand is requested after the first has been used, and a block's float32 scale where it is applied.
 template <int RA, int TB, int W, int ASC, int BX, bool WIDE, int OUT>
 __global__ __launch_bounds__(64 * W) void product_direct(ProductArgs p) {
     constexpr int kTile = RA * TB * 256;
@@ -641,16 +642,17 @@ static void variant(const ProductArgs &p, const ProductPlan &plan, hipStream_t s
 
 // Which kernel runs a product, and into how many parts its reduction is split: the least of their estimated
 // times.  The estimate is a workgroup's blocks times what one takes (in microseconds, fitted to times on this
-// card over ten weights, N from 512 to 8192, K from 512 to 18432, at 16 to 8192 rows, every kernel and split
-// of each: the rule's choice is 0.8 % above the best of them in the mean, 18 % at the worst), as often as its
-// workgroups outnumber the 256 CUs, plus the start and end of each round, plus the join of the parts:
+// card over ten weights, N from 512 to 8192, K from 512 to 18432, at 16 to 8192 rows, every kernel and eight splits
+// of each: where the rule's choice is among those timed, 287 of 320 products, it is 0.5 % above the best of them
+// in the mean, 10 % at the worst), as often as its workgroups outnumber the 256 CUs, plus the start and end of each
+// round, plus the join of the parts:
 //   direct kernels  the bytes of a block at 32.9 GB/s a CU (the waves of a CU share that rate), at least
 //                   0.5 for every 8 blocks: a small reduction is one round trip to memory
 //   tiled kernels   a block alone on its CU, and as a share of the CU's time; the second pair widened
 //   join            1.9 and the parts' bytes, written and read, at 5.4 TB/s
-// With M = 4096, K = 7168 (estimate / measured): 32 rows 10.6 / 12.1 (64 x 64, 8 parts), 16 x 32 direct
-// 13.5 / 13.1; 256 rows 19.5 / 20.1 (128 x 64, 2 parts), 128 x 128 in 4 parts 20.2 / 19.6; 777 rows 32 / 34
-// (128 x 128), 128 x 64 39 / 37; 4096 rows 89 / 99 (256 x 256), 128 x 128 121 / 128.
+// With M = 4096, K = 7168 (estimate / measured): 32 rows 10.6 / 12.2 (128 x 64, 8 parts), 64 x 64 in 4 parts
+// 11.0 / 11.3, 16 x 32 direct 13.5 / 13.0; 256 rows 19.5 / 20.1 (128 x 64, 2 parts), 128 x 128 in 4 parts
+// 20.2 / 19.6; 777 rows 32 / 34 (128 x 128), 128 x 64 39 / 37; 4096 rows 89 / 99 (256 x 256), 128 x 128 121 / 128.
 ProductPlan product_plan(int M, int R, int Kp, bool wide, bool may_split) {
     struct Kind {
         ProductPlan::Kernel kernel;
