@@ -637,6 +637,185 @@ ft_status_t ft_router_backward(const ft_balance_desc_t *desc, const float *logit
                                const float *d_loss, const float *topk_w, const float *d_topk_w, float *d_logits,
                                void *stream);
 
+/*
+ * ---- The routed experts in training: pairs sorted by expert into groups of rows, rows of tokens in that
+ * order and back, products over the groups with their gradients, and the norms around the block.
+ *
+ * A step over T tokens routed by ft_route_only:
+ *   forward    ft_expert_sort; ft_expert_gather (row form of x, its column form kept); ft_expert_linear (gate and up);
+ *              ft_swiglu_quantize over the rows; ft_expert_linear (down); ft_expert_combine with topk_w
+ *   backward   ft_expert_gather of dy with topk_w (both forms), ft_expert_gate_grad (the d_topk_w of
+ *              ft_router_backward); ft_expert_linear and ft_expert_weight_grad (down); ft_swiglu_backward over the rows;
+ *              ft_expert_linear and ft_expert_weight_grad (gate and up); ft_expert_combine without weights (dx)
+ *
+ * The rows' layout (host struct, read during the call only; the same for every call of a step):
+ *   n_experts, top_k   as in ft_moe_desc_t: 1..1024, 1..min(n_experts, 64)
+ *   first, local       the experts that are here, first .. first + local - 1 (all: 0, n_experts): where the experts are
+ *                      spread over GPUs, pairs of the others have no row
+ *   align              16 or 128: every group starts at a multiple of it.  Column forms, and so weight gradients,
+ *                      need 128 (their blocks of 128 rows must not meet two experts); 16 pads less
+ *   rows               capacity of the row buffers: a multiple of align from align to 1048576.
+ *                      ft_expert_sort_rows gives what T tokens need whatever their routing
+ * FT_ERR_SHAPE otherwise.  0 <= T <= 1048576; array pointers are 16-byte aligned except those of the tables, the gates
+ * and float32 scales; feature counts as for the dense calls above.
+ */
+typedef struct {
+    int32_t n_experts, top_k, first, local, align, rows;
+} ft_sort_desc_t;
+
+/*
+ * The tables (device pointers, caller-owned).  Group e = 0 .. local - 1 belongs to expert first + e.
+ *   row_pair [rows]     pair p = t * top_k + j of a row; -1: no pair (a group's padding, rows behind the last group)
+ *   pair_row [T*top_k]  row of a pair; -1: none (an expert that is not here, a masked token, no place)
+ *   off      [local+1]  group e is rows [off[e], off[e+1]), pairs first, in ascending order; off[local] ends the last
+ *   count    [local]    its rows with a pair
+ *   dropped  [1]        pairs of local experts that found no place: when the capacity is used up, the
+ *                       pairs left of that expert and all of the later ones
+ * The calls that read tables take what lies outside the ranges above as no pair, no row or no group.
+ */
+typedef struct {
+    int32_t *row_pair;
+    int32_t *pair_row;
+    int32_t *off;
+    int32_t *count;
+    int32_t *dropped;
+} ft_sort_t;
+
+/* Rows that hold every pair of T tokens whatever the routing (desc->rows is not read); 0 if desc or T is invalid or
+ * more than 1048576 would be needed. */
+int32_t ft_expert_sort_rows(const ft_sort_desc_t *desc, int32_t T);
+
+/*
+ * The tables of a routing.
+ *   topk_ids  [T][top_k] int32 (ft_route_t.topk_ids); an id that is not of a local expert has no row; an id that
+ *             occurs twice in a token has two
+ *   mask      [T] uint8 or NULL: a token with 0 has no rows (padding)
+ *   out       all overwritten, T == 0 included
+ *   ws        at least ft_expert_sort_workspace_bytes(desc, T) bytes (0 if desc is invalid)
+ */
+size_t ft_expert_sort_workspace_bytes(const ft_sort_desc_t *desc, int32_t max_tokens);
+ft_status_t ft_expert_sort(const ft_sort_desc_t *desc, const int32_t *topk_ids, int32_t T, const uint8_t *mask,
+                           const ft_sort_t *out, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * The tokens' rows in the order of the groups: row r of pair (t, j) is x[t], times weights[t][j] where weights is given
+ * (the gradient of ft_expert_combine); a group's padding is zeros; rows behind the last group are left as they were.
+ *   x        [T][C] in x_dtype (FT_DT_BF16 or FT_DT_F32)
+ *   weights  [T][top_k] float32 or NULL
+ *   plain    [rows][C] in plain_dtype (FT_DT_BF16 or FT_DT_F32), or NULL
+ *   row      row form of the rows (R = rows, K = C), or NULL;  col  their column form (R = C, K = rows; align 128), or
+ *            NULL.  At least one of the three.  Scale bytes past rows (row form) and C (column form) stand for nothing
+ *            and may be left as they were
+ * Reads sort->row_pair and sort->off.  T == 0 enqueues nothing.
+ */
+ft_status_t ft_expert_gather(const ft_sort_desc_t *desc, const ft_sort_t *sort, const void *x, int32_t x_dtype, int32_t T,
+                             int32_t C, const float *weights, void *plain, int32_t plain_dtype, const ft_act_codes_t *row,
+                             const ft_act_codes_t *col, void *stream);
+
+/*
+ * The rows back to their tokens: y[t] = base[t] + sum_j weights[t][j] rows[row of (t, j)], in float32 by ascending j,
+ * rounded once; pairs without a row add nothing.  Without weights it is the gradient of ft_expert_gather.
+ *   rows     [desc->rows][C] in rows_dtype, y and base [T][C] in y_dtype (FT_DT_BF16 or FT_DT_F32)
+ *   base     or NULL (zeros); may be y
+ * Reads sort->pair_row.  T == 0 enqueues nothing.
+ */
+ft_status_t ft_expert_combine(const ft_sort_desc_t *desc, const ft_sort_t *sort, const void *rows, int32_t rows_dtype,
+                              int32_t T, int32_t C, const float *weights, const void *base, void *y, int32_t y_dtype,
+                              void *stream);
+
+/*
+ * Gradient of the gates: d_weights[t][j] = sum_c dy[t][c] rows[row of (t, j)][c], 0 for pairs without a row.
+ *   rows [desc->rows][C] in rows_dtype, dy [T][C] in dy_dtype, d_weights [T][top_k] float32, overwritten
+ * Sums are float32 in a fixed order.  Reads sort->pair_row.  T == 0 enqueues nothing.
+ */
+ft_status_t ft_expert_gate_grad(const ft_sort_desc_t *desc, const ft_sort_t *sort, const void *rows, int32_t rows_dtype,
+                                const void *dy, int32_t dy_dtype, int32_t T, int32_t C, float *d_weights, void *stream);
+
+/*
+ * Products over the groups: y[r] = x[r] W_e^T for every row r with a pair of every group e, with ft_linear's
+ * formats, arithmetic and order of sums (one chunk, nothing is split).
+ *   linear    x_dtype must be FT_DT_FP8_ACT
+ *   w, w_scales   the local experts' weights, one behind the other, each in ft_linear's format:
+ *             [local][N][Kp] codes, [local][ceil(N/128)][Kp/128] float32
+ *   x         row form of the rows (R = rows, K = in_features); padding is not read
+ *   T         tokens of the routing: with them the call chooses its kernel and its grid
+ *   y         [rows][N] in y_dtype; a group's padding is zeros, rows behind the last group are left as they were
+ * Reads sort->off and sort->count.  The gradient of x is the same call on the transposed weights.  T == 0 enqueues nothing.
+ */
+ft_status_t ft_expert_linear(const ft_sort_desc_t *desc, const ft_linear_desc_t *linear, const uint8_t *w,
+                             const float *w_scales, const ft_act_codes_t *x, const ft_sort_t *sort, int32_t T, void *y,
+                             void *stream);
+
+/* ft_linear_transpose for n weights (1..1024) that lie one behind the other. */
+ft_status_t ft_expert_linear_transpose(int32_t n, int32_t out_features, int32_t in_features, const uint8_t *w,
+                                       const float *w_scales, uint8_t *wt, float *wt_scales, void *stream);
+
+/*
+ * Gradients of the weights: dw[e] = sum over the rows r of group e of dy[r]^T x[r], [local][N][K], as
+ * ft_linear_weight_grad; a group without rows gives zeros (accumulate: leaves its dw as it is).
+ *   dy_col, x_col   column forms of the rows (R = N or K, K = rows), align 128; a group's padding must be zeros
+ *             (ft_expert_gather and ft_expert_linear leave it so, and ft_swiglu_backward keeps it)
+ * Reads sort->off and sort->count.  T == 0 writes zeros (accumulate: leaves dw as it is).
+ */
+ft_status_t ft_expert_weight_grad(const ft_sort_desc_t *desc, int32_t out_features, int32_t in_features,
+                                  const ft_act_codes_t *dy_col, const ft_act_codes_t *x_col, const ft_sort_t *sort,
+                                  int32_t T, void *dw, int32_t dw_dtype, int32_t accumulate, void *stream);
+
+/*
+ * Norms before and after a block, with the block's gates and residual scale.  With rms(v) = sqrt(mean v^2 + eps) over a
+ * token's channels:
+ *   u = post b / rms(b) (post_norm 1) or b (post_norm 0),  r = x + scale gate_c token_gate_t u,  n = pre r / rms(r)
+ *   channels   C; x_dtype of x, r and their gradients, y_dtype of b, n and theirs, w_dtype of pre, post and gate
+ *              (FT_DT_BF16 or FT_DT_F32 each);  eps >= 0 and scale finite (FT_ERR_SHAPE otherwise)
+ *   params     pre, post, gate [C], token_gate [T] float32; NULL: ones
+ * Everything is computed in float32 and rounded once: n is of r before r's rounding.
+ */
+typedef struct {
+    int32_t channels, x_dtype, y_dtype, w_dtype, post_norm;
+    float eps, scale;
+} ft_norm_desc_t;
+
+typedef struct {
+    const void *pre;
+    const void *post;
+    const void *gate;
+    const float *token_gate;
+} ft_norm_params_t;
+
+/*
+ *   x      [T][C]: the residual stream in front of the block;  block [T][C]: the block's output b, or NULL: r = x
+ *   r      [T][C]: the residual stream behind it, or NULL; may be x.  Not written without a block
+ *   n      [T][C], or NULL;  n_row  row form of n (the next product's input), or NULL.  One of r, n and n_row at least,
+ *          and n or n_row without a block
+ * T == 0 enqueues nothing.
+ */
+ft_status_t ft_block_norm(const ft_norm_desc_t *desc, const ft_norm_params_t *params, const void *x, const void *block,
+                          int32_t T, void *r, void *n, const ft_act_codes_t *n_row, void *stream);
+
+/* Gradients of params, all float32 [C] ([T] for token_gate), overwritten; NULL ones are left out. */
+typedef struct {
+    float *pre;
+    float *post;
+    float *gate;
+    float *token_gate;
+} ft_norm_grads_t;
+
+/*
+ * The backward pass, from r as ft_block_norm left it (x where there is no block), block, and the gradients of r and n:
+ *   dr, dn     [T][C]; either may be NULL (zeros), not both
+ *   dx         [T][C] in x_dtype, or NULL; may be dr.   d_block [T][C] in y_dtype, or NULL; may be dn
+ *   grads      or NULL.  d_block, post, gate and token_gate need block; pre needs dn; post needs post_norm
+ *              (FT_ERR_NULL otherwise)
+ *   ws         at least ft_block_norm_workspace_bytes(desc, T) bytes (0 if desc is invalid); may be NULL where none of pre,
+ *              post and gate is asked for
+ * Sums run in a fixed order, those over tokens in float32 within a workgroup and in float64 beyond.  T == 0 writes
+ * zeros into pre, post and gate.
+ */
+size_t ft_block_norm_workspace_bytes(const ft_norm_desc_t *desc, int32_t max_tokens);
+ft_status_t ft_block_norm_backward(const ft_norm_desc_t *desc, const ft_norm_params_t *params, const void *r,
+                                   const void *block, const void *dr, const void *dn, int32_t T, void *dx, void *d_block,
+                                   const ft_norm_grads_t *grads, void *ws, size_t ws_bytes, void *stream);
+
 /* Static string for a status code. */
 const char *ft_status_string(ft_status_t status);
 

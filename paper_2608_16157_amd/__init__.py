@@ -30,12 +30,24 @@ of the C ABI declared in ``include/ftmoe.h``:
     ft_balance_loss(desc, logits, topk_ids, T, out, ws, seq_off=None, mask=None, stream=None)
     ft_router_backward(desc, logits, topk_ids, T, balance, d_loss, d_logits, topk_w=None, d_topk_w=None,
                        seq_off=None, mask=None, stream=None)
+    ft_expert_sort_rows(desc, T) -> int;  ft_expert_sort_workspace_bytes(desc, max_tokens) -> int
+    ft_expert_sort(desc, topk_ids, T, out, ws, mask=None, stream=None)
+    ft_expert_gather(desc, sort, x, T, C, weights=None, rows=None, row=None, col=None, stream=None)
+    ft_expert_combine(desc, sort, rows, T, C, y, weights=None, base=None, stream=None)
+    ft_expert_gate_grad(desc, sort, rows, dy, T, C, d_weights, stream=None)
+    ft_expert_linear(desc, linear, weight, x, sort, T, y, stream=None)
+    ft_expert_linear_transpose(n, out_features, in_features, weight, weight_t, stream=None)
+    ft_expert_weight_grad(desc, out_features, in_features, dy_col, x_col, sort, T, dw, accumulate=False, stream=None)
+    ft_block_norm(desc, params, x, block, T, r=None, n=None, n_row=None, stream=None)
+    ft_block_norm_workspace_bytes(desc, max_tokens) -> int
+    ft_block_norm_backward(desc, params, r, block, dr, dn, T, dx=None, d_block=None, grads=None, ws=None, stream=None)
     ft_status_string(status) -> str
 
 ``desc`` is a dict with the ft_moe_desc_t fields; ``route`` a RouteBuffers; ``banks`` a dict
 with w13, w2 (and s13, s2 for fp8) device tensors; a ``weight`` of the dense product a dict with w and
-s; 8-bit forms ActCodes; ``ft_balance_loss``'s outputs a BalanceBuffers; everything else device
-tensors.  A non-OK status raises FtError.  If the library is not built, importing works but every call raises.
+s; 8-bit forms ActCodes; ``ft_balance_loss``'s outputs a BalanceBuffers; the ``desc`` of the ft_expert calls a dict
+with the ft_sort_desc_t fields and ``sort`` a SortBuffers; the ``desc`` of the norms one with the ft_norm_desc_t
+fields, ``params`` and ``grads`` dicts of pre, post, gate and token_gate; everything else device tensors.  A non-OK status raises FtError.  If the library is not built, importing works but every call raises.
 """
 from __future__ import annotations
 
@@ -62,7 +74,10 @@ EXPORTED = ("ft_moe_workspace_bytes", "ft_route_only", "ft_moe_forward", "ft_moe
             "ft_cache_fill", "ft_moe_step_hybrid", "ft_prefill_layers", "ft_status_string",
             "ft_cpu_pool_create", "ft_cpu_pool_destroy", "ft_act_quantize", "ft_linear_workspace_bytes",
             "ft_linear", "ft_linear_transpose", "ft_linear_weight_grad", "ft_swiglu_quantize",
-            "ft_swiglu_backward", "ft_balance_workspace_bytes", "ft_balance_loss", "ft_router_backward")
+            "ft_swiglu_backward", "ft_balance_workspace_bytes", "ft_balance_loss", "ft_router_backward",
+            "ft_expert_sort_rows", "ft_expert_sort_workspace_bytes", "ft_expert_sort", "ft_expert_gather",
+            "ft_expert_combine", "ft_expert_gate_grad", "ft_expert_linear", "ft_expert_linear_transpose",
+            "ft_expert_weight_grad", "ft_block_norm", "ft_block_norm_workspace_bytes", "ft_block_norm_backward")
 FT_PROF_STAGES = 4
 FT_NOALLOC_SCRATCH_BYTES = 64 << 20
 
@@ -136,6 +151,27 @@ class ft_balance_desc_t(ctypes.Structure):
 
 class ft_balance_t(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("counts", "tokens", "prob", "frac", "loss")]
+
+
+class ft_sort_desc_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_experts", "top_k", "first", "local", "align", "rows")]
+
+
+class ft_sort_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("row_pair", "pair_row", "off", "count", "dropped")]
+
+
+class ft_norm_desc_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("channels", "x_dtype", "y_dtype", "w_dtype", "post_norm")] + \
+               [("eps", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
+class ft_norm_params_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("pre", "post", "gate", "token_gate")]
+
+
+class ft_norm_grads_t(ctypes.Structure):
+    _fields_ = ft_norm_params_t._fields_
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -218,6 +254,24 @@ def load(path: str = None) -> ctypes.CDLL:
     lib.ft_balance_loss.argtypes = [P(ft_balance_desc_t), p, p, i, p, p, bal, p, z, p]
     lib.ft_router_backward.restype = ctypes.c_int
     lib.ft_router_backward.argtypes = [P(ft_balance_desc_t), p, p, i, p, p, bal, p, p, p, p, p]
+    sd, st, ld, nd = P(ft_sort_desc_t), P(ft_sort_t), P(ft_linear_desc_t), P(ft_norm_desc_t)
+    lib.ft_expert_sort_rows.restype = i
+    lib.ft_expert_sort_rows.argtypes = [sd, i]
+    lib.ft_expert_sort_workspace_bytes.restype = z
+    lib.ft_expert_sort_workspace_bytes.argtypes = [sd, i]
+    lib.ft_block_norm_workspace_bytes.restype = z
+    lib.ft_block_norm_workspace_bytes.argtypes = [nd, i]
+    for name, args in (("ft_expert_sort", [sd, p, i, p, st, p, z, p]),
+                       ("ft_expert_gather", [sd, st, p, i, i, i, p, p, i, codes, codes, p]),
+                       ("ft_expert_combine", [sd, st, p, i, i, i, p, p, p, i, p]),
+                       ("ft_expert_gate_grad", [sd, st, p, i, p, i, i, i, p, p]),
+                       ("ft_expert_linear", [sd, ld, p, p, codes, st, i, p, p]),
+                       ("ft_expert_linear_transpose", [i, i, i, p, p, p, p, p]),
+                       ("ft_expert_weight_grad", [sd, i, i, codes, codes, st, i, p, i, i, p]),
+                       ("ft_block_norm", [nd, P(ft_norm_params_t), p, p, i, p, p, codes, p]),
+                       ("ft_block_norm_backward", [nd, P(ft_norm_params_t), p, p, p, p, i, p, p, P(ft_norm_grads_t), p, z, p])):
+        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).argtypes = args
     lib.ft_status_string.restype = ctypes.c_char_p
     lib.ft_status_string.argtypes = [ctypes.c_int]
     _lib = lib
@@ -1001,3 +1055,282 @@ def ft_router_backward(desc: dict, logits: torch.Tensor, topk_ids: Optional[torc
         dev, dw = _arg(dev, d_topk_w, "d_topk_w", _F32, T * d.top_k)
     st = _on(dev, load().ft_router_backward, ctypes.byref(d), lp, ip, T, sp, mp, bp, dl, wp, dw, op, stream)
     _check(st, "ft_router_backward")
+
+
+# ------------------------------------------------------------ the routed experts in training, and norms
+
+@functools.lru_cache(maxsize=256)
+def _sort_struct(*values: int) -> ft_sort_desc_t:
+    return ft_sort_desc_t(*values)
+
+
+def _sort_desc(d: dict) -> ft_sort_desc_t:
+    """``first`` and ``local`` may be left out (every expert is here)."""
+    E = int(d["n_experts"])
+    return _sort_struct(E, int(d["top_k"]), int(d.get("first", 0)), int(d.get("local", E)), int(d["align"]), int(d["rows"]))
+
+
+def ft_expert_sort_rows(desc: dict, T: int) -> int:
+    """Rows that hold every pair of T tokens (``rows`` is not needed in ``desc``); 0 where the library refuses."""
+    return int(load().ft_expert_sort_rows(ctypes.byref(_sort_desc({"rows": 0, **desc})), int(T)))
+
+
+class SortBuffers:
+    """Device tensors behind one ft_sort_t for T tokens: row_pair [rows], pair_row [T][top_k], off [local + 1],
+    count [local], dropped [1], all int32."""
+
+    def __init__(self, desc: dict, T: int, device="cuda"):
+        d = _sort_desc(desc)
+        kw = dict(dtype=torch.int32, device=device)
+        self.row_pair = torch.empty(d.rows, **kw)
+        self.pair_row = torch.empty(T, d.top_k, **kw)
+        self.off = torch.empty(d.local + 1, **kw)
+        self.count = torch.empty(d.local, **kw)
+        self.dropped = torch.empty(1, **kw)
+
+    @classmethod
+    def of(cls, row_pair, pair_row, off, count, dropped) -> "SortBuffers":
+        """Buffers over existing tensors."""
+        self = cls.__new__(cls)
+        self.row_pair, self.pair_row, self.off, self.count, self.dropped = row_pair, pair_row, off, count, dropped
+        return self
+
+
+def ft_expert_sort_workspace_bytes(desc: dict, max_tokens: int) -> int:
+    return int(load().ft_expert_sort_workspace_bytes(ctypes.byref(_sort_desc(desc)), int(max_tokens)))
+
+
+def alloc_sort_workspace(desc: dict, max_tokens: int, device="cuda") -> torch.Tensor:
+    """Workspace of ft_expert_sort for up to max_tokens tokens."""
+    n = ft_expert_sort_workspace_bytes(desc, max_tokens)
+    if n == 0:
+        raise FtError(FT_ERR_SHAPE, "ft_expert_sort_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _need_tokens(d: ft_sort_desc_t, T: int, *features: int) -> None:
+    _need_sizes(T, *features)
+    if d.rows < 16 or d.top_k < 1 or d.local < 1:
+        raise FtError(FT_ERR_SHAPE, "sizes")
+
+
+def _sort_arg(dev: int, d: ft_sort_desc_t, T: int, sort, names):
+    """The tables ``names`` of a SortBuffers as an ft_sort_t, the others left out."""
+    if not isinstance(sort, SortBuffers):
+        raise ValueError(f"sort: expected a SortBuffers, got {type(sort).__name__}")
+    out = ft_sort_t()
+    for n in names:
+        size = {"row_pair": d.rows, "pair_row": T * d.top_k, "off": d.local + 1, "count": d.local, "dropped": 1}[n]
+        dev, at = _arg(dev, getattr(sort, n), n, _I32, size)
+        setattr(out, n, at)
+    return dev, ctypes.byref(out)
+
+
+def _optional(dev: int, t, name: str, dtypes: tuple, numel: int):
+    return (dev, None) if t is None else _arg(dev, t, name, dtypes, numel)
+
+
+def ft_expert_sort(desc: dict, topk_ids: torch.Tensor, T: int, out: SortBuffers, ws: torch.Tensor,
+                   mask: Optional[torch.Tensor] = None, stream=None) -> None:
+    """``topk_ids``: the routing's (RouteBuffers.topk_ids); ``mask``: uint8 or bool per token."""
+    d, T = _sort_desc(desc), int(T)
+    _need_tokens(d, T)
+    dev, ip, mp = -1, None, None
+    if T > 0:
+        dev, ip = _arg(dev, topk_ids, "topk_ids", _I32, T * d.top_k)
+        dev, mp = _optional(dev, mask, "mask", _MASKS, T)
+    dev, sp = _sort_arg(dev, d, T, out, ("row_pair", "pair_row", "off", "count", "dropped") if T else
+                        ("row_pair", "off", "count", "dropped"))
+    dev, wp = _arg(dev, ws, "ws", _BYTES, 0)
+    st = _on(dev, load().ft_expert_sort, ctypes.byref(d), ip, T, mp, sp, wp, ws.numel(), stream)
+    _check(st, "ft_expert_sort")
+
+
+def ft_expert_gather(desc: dict, sort: SortBuffers, x: torch.Tensor, T: int, C: int,
+                     weights: Optional[torch.Tensor] = None, rows: Optional[torch.Tensor] = None,
+                     row: Optional[ActCodes] = None, col: Optional[ActCodes] = None, stream=None) -> None:
+    """``rows``: the plain rows, float32 or bfloat16 [desc rows][C]; ``row``, ``col``: their 8-bit forms."""
+    d, T, C = _sort_desc(desc), int(T), int(C)
+    _need_tokens(d, T, C)
+    if T == 0:
+        return
+    dev, xp = _arg(-1, x, "x", _FLOAT_TYPES, T * C)
+    dev, sp = _sort_arg(dev, d, T, sort, ("row_pair", "off"))
+    dev, wp = _optional(dev, weights, "weights", _F32, T * d.top_k)
+    dev, pp = _optional(dev, rows, "rows", _FLOAT_TYPES, d.rows * C)
+    dev, rp = _codes_arg(dev, row, "row", d.rows, C, True)
+    dev, cp = _codes_arg(dev, col, "col", C, d.rows, True)
+    st = _on(dev, load().ft_expert_gather, ctypes.byref(d), sp, xp, _FLOATS[x.dtype], T, C, wp, pp,
+             0 if rows is None else _FLOATS[rows.dtype], rp, cp, stream)
+    _check(st, "ft_expert_gather")
+
+
+def ft_expert_combine(desc: dict, sort: SortBuffers, rows: torch.Tensor, T: int, C: int, y: torch.Tensor,
+                      weights: Optional[torch.Tensor] = None, base: Optional[torch.Tensor] = None, stream=None) -> None:
+    """``base``: of y's type, or y itself."""
+    d, T, C = _sort_desc(desc), int(T), int(C)
+    _need_tokens(d, T, C)
+    if T == 0:
+        return
+    dev, rp = _arg(-1, rows, "rows", _FLOAT_TYPES, d.rows * C)
+    dev, sp = _sort_arg(dev, d, T, sort, ("pair_row",))
+    dev, yp = _arg(dev, y, "y", _FLOAT_TYPES, T * C)
+    dev, wp = _optional(dev, weights, "weights", _F32, T * d.top_k)
+    dev, bp = _optional(dev, base, "base", (y.dtype,), T * C)
+    st = _on(dev, load().ft_expert_combine, ctypes.byref(d), sp, rp, _FLOATS[rows.dtype], T, C, wp, bp, yp,
+             _FLOATS[y.dtype], stream)
+    _check(st, "ft_expert_combine")
+
+
+def ft_expert_gate_grad(desc: dict, sort: SortBuffers, rows: torch.Tensor, dy: torch.Tensor, T: int, C: int,
+                        d_weights: torch.Tensor, stream=None) -> None:
+    d, T, C = _sort_desc(desc), int(T), int(C)
+    _need_tokens(d, T, C)
+    if T == 0:
+        return
+    dev, rp = _arg(-1, rows, "rows", _FLOAT_TYPES, d.rows * C)
+    dev, sp = _sort_arg(dev, d, T, sort, ("pair_row",))
+    dev, yp = _arg(dev, dy, "dy", _FLOAT_TYPES, T * C)
+    dev, wp = _arg(dev, d_weights, "d_weights", _F32, T * d.top_k)
+    st = _on(dev, load().ft_expert_gate_grad, ctypes.byref(d), sp, rp, _FLOATS[rows.dtype], yp, _FLOATS[dy.dtype], T, C, wp,
+             stream)
+    _check(st, "ft_expert_gate_grad")
+
+
+def _expert_weights(dev: int, weight: dict, name: str, n: int, N: int, K: int):
+    kp = _pad128(K)
+    dev, w = _arg(dev, weight.get("w"), name + "['w']", _CODES, n * N * kp)
+    dev, s = _arg(dev, weight.get("s"), name + "['s']", _F32, n * (_pad128(N) // 128) * (kp // 128))
+    return dev, w, s
+
+
+def ft_expert_linear(desc: dict, linear: dict, weight: dict, x: ActCodes, sort: SortBuffers, T: int, y: torch.Tensor,
+                     stream=None) -> None:
+    """``weight``: ``w`` [local][N][Kp] codes and ``s`` their block scales; ``x``: the row form of the rows."""
+    d, l, T = _sort_desc(desc), _linear_desc(linear), int(T)
+    N, K = l.out_features, l.in_features
+    _need_tokens(d, T, N, K)
+    if T == 0:
+        return
+    if l.x_dtype != FT_DT_FP8_ACT or l.y_dtype not in _X_DTYPES:
+        raise FtError(FT_ERR_DTYPE, "ft_expert_linear")
+    dev, w, s = _expert_weights(-1, weight, "weight", d.local, N, K)
+    dev, xp = _codes_arg(dev, x, "x", d.rows, K)
+    dev, sp = _sort_arg(dev, d, T, sort, ("off", "count"))
+    dev, yp = _arg(dev, y, "y", (_X_DTYPES[l.y_dtype],), d.rows * N)
+    st = _on(dev, load().ft_expert_linear, ctypes.byref(d), ctypes.byref(l), w, s, xp, sp, T, yp, stream)
+    _check(st, "ft_expert_linear")
+
+
+def ft_expert_linear_transpose(n: int, out_features: int, in_features: int, weight: dict, weight_t: dict, stream=None) -> None:
+    n, N, K = int(n), int(out_features), int(in_features)
+    _need_sizes(0, N, K)
+    if not 1 <= n <= 1024:
+        raise FtError(FT_ERR_SHAPE, "sizes")
+    dev, w, s = _expert_weights(-1, weight, "weight", n, N, K)
+    dev, wt, ts = _expert_weights(dev, weight_t, "weight_t", n, K, N)
+    st = _on(dev, load().ft_expert_linear_transpose, n, N, K, w, s, wt, ts, stream)
+    _check(st, "ft_expert_linear_transpose")
+
+
+def ft_expert_weight_grad(desc: dict, out_features: int, in_features: int, dy_col: ActCodes, x_col: ActCodes,
+                          sort: SortBuffers, T: int, dw: torch.Tensor, accumulate: bool = False, stream=None) -> None:
+    """``dw``: float32 or bfloat16 [local][out_features][in_features]."""
+    d, N, K, T = _sort_desc(desc), int(out_features), int(in_features), int(T)
+    _need_tokens(d, T, N, K)
+    dev, out = _arg(-1, dw, "dw", _FLOAT_TYPES, d.local * N * K)
+    yp = xp = sp = None
+    if T > 0:
+        dev, yp = _codes_arg(dev, dy_col, "dy_col", N, d.rows)
+        dev, xp = _codes_arg(dev, x_col, "x_col", K, d.rows)
+        dev, sp = _sort_arg(dev, d, T, sort, ("off", "count"))
+    st = _on(dev, load().ft_expert_weight_grad, ctypes.byref(d), N, K, yp, xp, sp, T, out, _FLOATS[dw.dtype],
+             1 if accumulate else 0, stream)
+    _check(st, "ft_expert_weight_grad")
+
+
+@functools.lru_cache(maxsize=256)
+def _norm_struct(*values) -> ft_norm_desc_t:
+    return ft_norm_desc_t(*values)
+
+
+def _norm_desc(d: dict) -> ft_norm_desc_t:
+    return _norm_struct(int(d["channels"]), int(d["x_dtype"]), int(d["y_dtype"]), int(d["w_dtype"]), int(d.get("post_norm", 0)),
+                        float(d["eps"]), float(d.get("scale", 1.0)))
+
+
+def _norm_types(d: ft_norm_desc_t, T: int, where: str):
+    """-> the tensor types of x, y and the weights."""
+    _need_sizes(T, d.channels)
+    kinds = [_X_DTYPES.get(v) for v in (d.x_dtype, d.y_dtype, d.w_dtype)]
+    if None in kinds:
+        raise FtError(FT_ERR_DTYPE, where)
+    return kinds
+
+
+def _norm_params(dev: int, d: ft_norm_desc_t, T: int, params: dict, kind):
+    out = ft_norm_params_t()
+    for n in ("pre", "post", "gate"):
+        dev, at = _optional(dev, params.get(n), n, (kind,), d.channels)
+        setattr(out, n, at)
+    dev, out.token_gate = _optional(dev, params.get("token_gate"), "token_gate", _F32, T)
+    return dev, ctypes.byref(out)
+
+
+def ft_block_norm(desc: dict, params: dict, x: torch.Tensor, block: Optional[torch.Tensor], T: int,
+                  r: Optional[torch.Tensor] = None, n: Optional[torch.Tensor] = None, n_row: Optional[ActCodes] = None,
+                  stream=None) -> None:
+    """``params``: ``pre``, ``post``, ``gate``, ``token_gate``, each a tensor or left out (ones)."""
+    d, T = _norm_desc(desc), int(T)
+    xk, yk, wk = _norm_types(d, T, "ft_block_norm")
+    if T == 0:
+        return
+    size = T * d.channels
+    dev, xp = _arg(-1, x, "x", (xk,), size)
+    dev, pp = _norm_params(dev, d, T, params, wk)
+    dev, bp = _optional(dev, block, "block", (yk,), size)
+    dev, rp = _optional(dev, r, "r", (xk,), size)
+    dev, np_ = _optional(dev, n, "n", (yk,), size)
+    dev, cp = _codes_arg(dev, n_row, "n_row", T, d.channels, True)
+    st = _on(dev, load().ft_block_norm, ctypes.byref(d), pp, xp, bp, T, rp, np_, cp, stream)
+    _check(st, "ft_block_norm")
+
+
+def ft_block_norm_workspace_bytes(desc: dict, max_tokens: int) -> int:
+    return int(load().ft_block_norm_workspace_bytes(ctypes.byref(_norm_desc(desc)), int(max_tokens)))
+
+
+def alloc_block_norm_workspace(desc: dict, max_tokens: int, device="cuda") -> torch.Tensor:
+    """Workspace of ft_block_norm_backward for up to max_tokens tokens."""
+    n = ft_block_norm_workspace_bytes(desc, max_tokens)
+    if n == 0:
+        raise FtError(FT_ERR_SHAPE, "ft_block_norm_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def ft_block_norm_backward(desc: dict, params: dict, r: torch.Tensor, block: Optional[torch.Tensor],
+                           dr: Optional[torch.Tensor], dn: Optional[torch.Tensor], T: int,
+                           dx: Optional[torch.Tensor] = None, d_block: Optional[torch.Tensor] = None,
+                           grads: Optional[dict] = None, ws: Optional[torch.Tensor] = None, stream=None) -> None:
+    """``grads``: float32 tensors for the gradients of ``params``, those left out or None are not formed."""
+    d, T = _norm_desc(desc), int(T)
+    xk, yk, wk = _norm_types(d, T, "ft_block_norm_backward")
+    size, g, dev = T * d.channels, ft_norm_grads_t(), -1
+    for n in ("pre", "post", "gate", "token_gate"):
+        dev, at = _optional(dev, (grads or {}).get(n), "d_" + n, _F32, T if n == "token_gate" else d.channels)
+        setattr(g, n, at)
+    if T == 0 and not (g.pre or g.post or g.gate):
+        return
+    dev, pp = _norm_params(dev, d, T, params, wk)
+    rp = bp = drp = dnp = dxp = dbp = None
+    if T > 0:
+        dev, rp = _arg(dev, r, "r", (xk,), size)
+        dev, bp = _optional(dev, block, "block", (yk,), size)
+        dev, drp = _optional(dev, dr, "dr", (xk,), size)
+        dev, dnp = _optional(dev, dn, "dn", (yk,), size)
+        dev, dxp = _optional(dev, dx, "dx", (xk,), size)
+        dev, dbp = _optional(dev, d_block, "d_block", (yk,), size)
+    dev, wp = _optional(dev, ws, "ws", _BYTES, 0)
+    st = _on(dev, load().ft_block_norm_backward, ctypes.byref(d), pp, rp, bp, drp, dnp, T, dxp, dbp, ctypes.byref(g), wp,
+             0 if ws is None else ws.numel(), stream)
+    _check(st, "ft_block_norm_backward")

@@ -173,7 +173,7 @@ ft_status_t ft_linear_transpose(int32_t out_features, int32_t in_features, const
     if (!w || !w_scales || !wt || !wt_scales) return FT_ERR_NULL;
     if (!aligned(w) || !aligned(wt) || reinterpret_cast<uintptr_t>(w_scales) % 4 || reinterpret_cast<uintptr_t>(wt_scales) % 4)
         return FT_ERR_SHAPE;
-    return launch_weight_transpose(w, w_scales, wt, wt_scales, out_features, in_features, static_cast<hipStream_t>(stream)) ==
+    return launch_weight_transpose(w, w_scales, wt, wt_scales, 1, out_features, in_features, static_cast<hipStream_t>(stream)) ==
                    hipSuccess
                ? FT_OK
                : FT_ERR_HIP;

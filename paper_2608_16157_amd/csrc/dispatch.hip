@@ -1,0 +1,234 @@
+// Rows of tokens in the order of the groups (ft_expert_gather), back to their tokens (ft_expert_combine), and the
+// gradient of the gates (ft_expert_gate_grad).  row_pair and pair_row come from sort.hip; what lies outside their
+// ranges counts as no pair and no row.
+//
+// All of these move memory once and compute little: the bound is HBM.
+#include "act_tile.h"
+
+namespace ftmoe {
+
+// The token of a row and the factor of its values: (-1, 0) where the row has no pair.
+__device__ __forceinline__ int row_token(const RowsArgs &a, long row, float &w) {
+    const int p = a.row_pair[row];
+    w = 1.0f;
+    if (static_cast<uint32_t>(p) >= static_cast<uint32_t>(a.T) * static_cast<uint32_t>(a.k)) return -1;
+    if (a.w) w = a.w[p];
+    return p / a.k;
+}
+// one past the last group's rows
+__device__ __forceinline__ int rows_end(const RowsArgs &a) { return min(a.off[a.n], a.rows); }
+
+__device__ __forceinline__ void store8(uint16_t *p, const float *v) {
+    uint4 o;
+    o.x = f32_to_bf16_any(v[0]) | f32_to_bf16_any(v[1]) << 16;
+    o.y = f32_to_bf16_any(v[2]) | f32_to_bf16_any(v[3]) << 16;
+    o.z = f32_to_bf16_any(v[4]) | f32_to_bf16_any(v[5]) << 16;
+    o.w = f32_to_bf16_any(v[6]) | f32_to_bf16_any(v[7]) << 16;
+    *reinterpret_cast<uint4 *>(p) = o;
+}
+__device__ __forceinline__ void store8(float *p, const float *v) {
+    reinterpret_cast<float4 *>(p)[0] = float4{v[0], v[1], v[2], v[3]};
+    reinterpret_cast<float4 *>(p)[1] = float4{v[4], v[5], v[6], v[7]};
+}
+
+// Plain rows: one wave per row.
+template <class XT, class OT>
+__global__ __launch_bounds__(256) void gather_plain(RowsArgs a, const XT *x, OT *out) {
+    const long row = static_cast<long>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    if (row >= rows_end(a)) return;
+    float w;
+    const int t = row_token(a, row, w);
+    const XT *from = x + static_cast<size_t>(max(t, 0)) * a.C;
+    OT *to = out + static_cast<size_t>(row) * a.C;
+#pragma unroll 4
+    for (int c = 8 * lane_id(); c < a.C; c += 512) {
+        float v[8];
+        load8(from + c, v);
+        zero_unless(t >= 0, v);
+        if (a.w)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[q] *= w;
+        store8(to + c, v);
+    }
+}
+
+// The row form alone: 8 lanes per (row, block of 128), two rows on the way at once.
+template <class XT>
+__global__ __launch_bounds__(256) void gather_rows(RowsArgs a, const XT *x, ActForm f) {
+    const int sub = threadIdx.x % 8, kb = blockIdx.x, c = kb * 128 + 16 * sub, end = rows_end(a);
+    const long row0 = static_cast<long>(blockIdx.y) * 64 + threadIdx.x / 8;
+    if (blockIdx.y * 64L >= end) return;
+    float v[2][16], w[2];
+    int t[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) t[r] = row_token(a, min(row0 + 32 * r, end - 1L), w[r]);
+#pragma unroll
+    for (int r = 0; r < 2; ++r) load16(x + static_cast<size_t>(max(t[r], 0)) * a.C + min(c, a.C - 16), v[r]);
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        quiet(v[r]);
+        if (a.w)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) v[r][q] *= w[r];
+        zero_unless(t[r] >= 0 && c < a.C, v[r]);   // C is a multiple of 16
+        if (row0 + 32 * r < end) put_row(v[r], f, row0 + 32 * r, end, kb, sub);
+    }
+}
+
+// Both forms, or the column form alone: one 128 x 128 tile per workgroup; groups start at multiples of 128.
+template <class XT>
+__global__ __launch_bounds__(kActThreads) void gather_tiles(RowsArgs a, const XT *x, ActForm row, ActForm col) {
+    __shared__ __attribute__((aligned(16))) ActTileShared<1> sh;
+    const int g = threadIdx.x / 16, sub = threadIdx.x % 16;
+    const int cb = blockIdx.x, rb = blockIdx.y, row0 = rb * 128 + kActRows * g, c = cb * 128 + 8 * sub;
+    if (rb * 128 >= rows_end(a)) return;
+    float v[1][kActRows][8], w[kActRows];
+    int t[kActRows];
+#pragma unroll
+    for (int r = 0; r < kActRows; ++r) t[r] = row_token(a, row0 + r, w[r]);
+#pragma unroll
+    for (int r = 0; r < kActRows; ++r) load8(x + static_cast<size_t>(max(t[r], 0)) * a.C + min(c, a.C - 8), v[0][r]);
+#pragma unroll
+    for (int r = 0; r < kActRows; ++r) {
+        quiet(v[0][r]);
+        if (a.w)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[0][r][q] *= w[r];
+        zero_unless(t[r] >= 0 && c < a.C, v[0][r]);   // C is a multiple of 16
+    }
+    const ActPlane to[1] = {{row, cb, col, cb * 128}};
+    put_tile<1>(v, sh, to, rb * 128, rb);
+}
+
+template <class XT>
+static void gather(const RowsArgs &a, const XT *x, void *plain, bool plain_f32, const ActForm &row, const ActForm &col,
+                   hipStream_t s) {
+    if (plain) {
+        const dim3 grid((a.rows + 3) / 4);
+        if (plain_f32)
+            hipLaunchKernelGGL((gather_plain<XT, float>), grid, dim3(256), 0, s, a, x, static_cast<float *>(plain));
+        else
+            hipLaunchKernelGGL((gather_plain<XT, uint16_t>), grid, dim3(256), 0, s, a, x, static_cast<uint16_t *>(plain));
+    }
+    const unsigned nkb = (a.C + 127) / 128;
+    if (col.codes)
+        hipLaunchKernelGGL(gather_tiles<XT>, dim3(nkb, a.rows / 128), dim3(kActThreads), 0, s, a, x, row, col);
+    else if (row.codes)
+        hipLaunchKernelGGL(gather_rows<XT>, dim3(nkb, (a.rows + 63) / 64), dim3(256), 0, s, a, x, row);
+}
+
+hipError_t launch_gather(const RowsArgs &a, const void *x, bool x_f32, void *plain, bool plain_f32, const ActForm &row,
+                         const ActForm &col, hipStream_t s) {
+    if (x_f32) gather(a, static_cast<const float *>(x), plain, plain_f32, row, col, s);
+    else gather(a, static_cast<const uint16_t *>(x), plain, plain_f32, row, col, s);
+    return hipGetLastError();
+}
+
+// y[t] = base[t] + sum_j w_tj rows[row of (t, j)], ascending j, in float32.  A thread holds 8 channels of a token; the
+// rows of 8 pairs are on the way at once.
+constexpr int kPairsOnWay = 8;
+
+template <class RT, class YT>
+__global__ __launch_bounds__(256) void combine_rows(RowsArgs a, const RT *rows, const YT *base, YT *y, int cblocks) {
+    const int t = blockIdx.x / cblocks, c = (blockIdx.x - t * cblocks) * 2048 + 8 * threadIdx.x;
+    if (c >= a.C) return;
+    float sum[8];
+    if (base) load8(base + static_cast<size_t>(t) * a.C + c, sum);
+    else
+#pragma unroll
+        for (int q = 0; q < 8; ++q) sum[q] = 0.0f;
+    const int32_t *at = a.pair_row + static_cast<size_t>(t) * a.k;
+    const float *w = a.w ? a.w + static_cast<size_t>(t) * a.k : nullptr;
+    for (int j0 = 0; j0 < a.k; j0 += kPairsOnWay) {
+        float v[kPairsOnWay][8];
+        bool in[kPairsOnWay];
+#pragma unroll
+        for (int j = 0; j < kPairsOnWay; ++j) {
+            const int row = at[min(j0 + j, a.k - 1)];
+            in[j] = j0 + j < a.k && static_cast<uint32_t>(row) < static_cast<uint32_t>(a.rows);
+            load8(rows + static_cast<size_t>(in[j] ? row : 0) * a.C + c, v[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < kPairsOnWay; ++j) {
+            if (!in[j]) continue;
+            const float f = w ? w[j0 + j] : 1.0f;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) sum[q] = fmaf(f, v[j][q], sum[q]);
+        }
+    }
+    store8(y + static_cast<size_t>(t) * a.C + c, sum);
+}
+
+hipError_t launch_combine(const RowsArgs &a, const void *rows, bool rows_f32, const void *base, void *y, bool y_f32, hipStream_t s) {
+    const int cblocks = (a.C + 2047) / 2048;
+    const dim3 grid(static_cast<unsigned>(a.T) * cblocks);
+    auto go = [&](auto *r, auto *o) {
+        using RT = std::remove_pointer_t<decltype(r)>;
+        using YT = std::remove_pointer_t<decltype(o)>;
+        hipLaunchKernelGGL((combine_rows<RT, YT>), grid, dim3(256), 0, s, a, static_cast<const RT *>(rows),
+                           static_cast<const YT *>(base), static_cast<YT *>(y), cblocks);
+    };
+    float *f = nullptr;
+    uint16_t *h = nullptr;
+    if (rows_f32) y_f32 ? go(f, f) : go(f, h);
+    else y_f32 ? go(h, f) : go(h, h);
+    return hipGetLastError();
+}
+
+// d_w[t][j] = <dy[t], rows[row of (t, j)]>, 0 without a row.  A workgroup of four waves per token, each every fourth
+// run of 512 channels; sums of a lane, of a wave and of the waves in a fixed order.
+template <class RT, class YT>
+__global__ __launch_bounds__(256) void gate_grad(RowsArgs a, const RT *rows, const YT *dy, float *d_w) {
+    __shared__ float part[4][kPairsOnWay];
+    const int t = blockIdx.x, wave = threadIdx.x / 64, lane = lane_id();
+    const int32_t *at = a.pair_row + static_cast<size_t>(t) * a.k;
+    const YT *d = dy + static_cast<size_t>(t) * a.C;
+    for (int j0 = 0; j0 < a.k; j0 += kPairsOnWay) {
+        const RT *from[kPairsOnWay];
+        bool in[kPairsOnWay];
+        float sum[kPairsOnWay];
+#pragma unroll
+        for (int j = 0; j < kPairsOnWay; ++j) {
+            const int row = at[min(j0 + j, a.k - 1)];
+            in[j] = j0 + j < a.k && static_cast<uint32_t>(row) < static_cast<uint32_t>(a.rows);
+            from[j] = rows + static_cast<size_t>(in[j] ? row : 0) * a.C;
+            sum[j] = 0.0f;
+        }
+        for (int c = 512 * wave + 8 * lane; c < a.C; c += 2048) {
+            float g[8], v[kPairsOnWay][8];
+            load8(d + c, g);
+#pragma unroll
+            for (int j = 0; j < kPairsOnWay; ++j) load8(from[j] + c, v[j]);
+#pragma unroll
+            for (int j = 0; j < kPairsOnWay; ++j)
+#pragma unroll
+                for (int q = 0; q < 8; ++q) sum[j] = fmaf(g[q], v[j][q], sum[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < kPairsOnWay; ++j) sum[j] = wave_sum_f32(sum[j]);
+        __syncthreads();   // the last pairs' parts have been read
+        if (lane == 0)
+#pragma unroll
+            for (int j = 0; j < kPairsOnWay; ++j) part[wave][j] = in[j] ? sum[j] : 0.0f;
+        __syncthreads();
+        const int j = threadIdx.x;
+        if (j < kPairsOnWay && j0 + j < a.k)
+            d_w[static_cast<size_t>(t) * a.k + j0 + j] = (part[0][j] + part[1][j]) + (part[2][j] + part[3][j]);
+    }
+}
+
+hipError_t launch_gate_grad(const RowsArgs &a, const void *rows, bool rows_f32, const void *dy, bool dy_f32, float *d_w, hipStream_t s) {
+    auto go = [&](auto *r, auto *o) {
+        using RT = std::remove_pointer_t<decltype(r)>;
+        using YT = std::remove_pointer_t<decltype(o)>;
+        hipLaunchKernelGGL((gate_grad<RT, YT>), dim3(a.T), dim3(256), 0, s, a, static_cast<const RT *>(rows),
+                           static_cast<const YT *>(dy), d_w);
+    };
+    float *f = nullptr;
+    uint16_t *h = nullptr;
+    if (rows_f32) dy_f32 ? go(f, f) : go(f, h);
+    else dy_f32 ? go(h, f) : go(h, h);
+    return hipGetLastError();
+}
+
+}  // namespace ftmoe

@@ -1,0 +1,174 @@
+// Products over groups of rows, one weight per group (ft_expert_linear, ft_expert_weight_grad): the tiles of
+// product_tile.h, each of which lies in one group.  The groups' sizes are known on the device only: the grid covers
+// the most tiles that the rows can make, a workgroup finds its tile from the groups' starts, and those without one end.
+//
+// ft_expert_linear: A is expert e's weight, B the rows of group e.  ft_expert_weight_grad: A and B are the column
+// forms of x and dy, whose blocks of 128 tokens lie in one group each, and the reduction runs over the group's.
+#include "product_tile.h"
+
+#include <algorithm>
+
+namespace ftmoe {
+
+// Group e as the tables have it, held inside the rows whatever they say.
+__device__ __forceinline__ int group_start(const GroupArgs &g, int e) {
+    return min(max(g.off[e], 0), g.rows) & -g.align;
+}
+
+struct GroupTile {
+    int e, row, real, end, total;   // expert, first row, one past its last row with a pair and past its last row; tiles in all
+};
+
+// Tile t of BB rows, in the order of the experts.  Every wave finds it for itself: 64 lanes hold up to 16 experts each.
+template <int BB>
+__device__ __forceinline__ void group_scan(const GroupArgs &g, uint32_t &before, uint32_t &upto, int &per) {
+    per = (g.n + 63) / 64;
+    const int e0 = min(lane_id() * per, g.n), e1 = min(e0 + per, g.n);
+    uint32_t sum = 0;
+    int o = group_start(g, e0);
+#pragma unroll 4
+    for (int e = e0; e < e1; ++e) {
+        const int next = group_start(g, e + 1);
+        sum += static_cast<uint32_t>(max(next - o, 0) + BB - 1) / BB;
+        o = next;
+    }
+    upto = wave_incl_scan_u32(sum);
+    before = upto - sum;
+}
+template <int BB>
+__device__ __forceinline__ GroupTile group_tile(const GroupArgs &g, uint32_t t, uint32_t before, uint32_t upto, int per) {
+    GroupTile r;
+    const int lane = __ffsll(static_cast<unsigned long long>(__ballot(t >= before && t < upto))) - 1;   // t is below the total
+    uint32_t rest = t - readlane_u32(before, lane);
+    r.e = lane * per;
+    for (;; ++r.e) {
+        r.row = group_start(g, r.e);
+        r.end = group_start(g, r.e + 1);
+        const uint32_t tiles = static_cast<uint32_t>(max(r.end - r.row, 0) + BB - 1) / BB;
+        if (rest < tiles) break;
+        rest -= tiles;
+    }
+    r.real = r.row + min(max(g.count[r.e], 0), max(r.end - r.row, 0));
+    r.row += static_cast<int>(rest) * BB;
+    r.end = min(r.end, r.row + BB);
+    return r;
+}
+
+// zeros in rows [b0, b1) and columns [a0, a1) of an output of M columns (a0, a1 and M multiples of 16)
+template <int OUT>
+__device__ __forceinline__ void zero_tile(void *out, int M, int a0, int a1, int b0, int b1) {
+    constexpr int kEach = OUT == 0 ? 8 : 4;
+    const int width = (a1 - a0) / kEach;
+    for (int i = threadIdx.x; i < (b1 - b0) * width; i += blockDim.x) {
+        const int b = b0 + i / width, a = a0 + i % width * kEach;
+        *reinterpret_cast<u32x4_t *>(static_cast<uint8_t *>(out) + (static_cast<size_t>(b) * M + a) * (OUT == 0 ? 2 : 4)) = u32x4_t{};
+    }
+}
+
+__device__ __forceinline__ ProductArgs of_expert(ProductArgs p, const GroupArgs &g, const GroupTile &t) {
+    p.a += t.e * g.a_stride;
+    p.as = static_cast<const float *>(p.as) + t.e * g.as_stride;
+    p.R = t.real;
+    return p;
+}
+
+template <int WA, int WB, int GA, int GB, bool WIDE, int OUT>
+__global__ __launch_bounds__(64 * GA * GB, 2) void expert_tiled(ProductArgs p, GroupArgs g, int na) {
+    constexpr int BA = 16 * WA * GA, BB = 16 * WB * GB;
+    uint32_t before, upto;
+    int per, ta, tb;
+    group_scan<BB>(g, before, upto, per);
+    const int nb = readlane_u32(upto, 63);
+    if (static_cast<int>(blockIdx.x) >= na * nb) return;
+    tile_at(xcd_remap(blockIdx.x, na * nb), na, nb, ta, tb);
+    const GroupTile t = group_tile<BB>(g, tb, before, upto, per);
+    if (t.row >= t.real) {
+        zero_tile<OUT>(p.out, p.M, ta * BA, min((ta + 1) * BA, p.M), t.row, t.end);
+        return;
+    }
+    lds_tile<WA, WB, GA, GB, 0, WIDE, OUT, true>(of_expert(p, g, t), ta * BA, t.row, 0, p.Kp / 128, t.end);
+}
+
+template <int RA, int TB, int W, bool WIDE, int OUT>
+__global__ __launch_bounds__(64 * W) void expert_direct(ProductArgs p, GroupArgs g) {
+    constexpr int BA = 16 * RA, BB = 16 * TB;
+    uint32_t before, upto;
+    int per;
+    group_scan<BB>(g, before, upto, per);
+    const uint32_t tb = blockIdx.y, ta = blockIdx.x;
+    if (tb >= readlane_u32(upto, 63)) return;
+    const GroupTile t = group_tile<BB>(g, tb, before, upto, per);
+    if (t.row >= t.real) {
+        zero_tile<OUT>(p.out, p.M, ta * BA, min(static_cast<int>(ta + 1) * BA, p.M), t.row, t.end);
+        return;
+    }
+    direct_tile<RA, TB, W, 0, 0, WIDE, OUT, true>(of_expert(p, g, t), ta * BA, t.row, 0, p.Kp / 128, t.end);
+}
+
+template <int WA, int WB, int GA, int GB, bool WIDE, int OUT>
+__global__ __launch_bounds__(64 * GA * GB, 2) void expert_grad(ProductArgs p, GroupArgs g, int na, int nb) {
+    constexpr int BA = 16 * WA * GA, BB = 16 * WB * GB;
+    const int L = xcd_remap(blockIdx.x, g.n * na * nb), e = L / (na * nb);
+    int ta, tb;
+    tile_at(L - e * (na * nb), na, nb, ta, tb);
+    int o = 0, blocks = 0;   // without tables there are no rows
+    if (g.off) {
+        o = group_start(g, e);
+        blocks = (min(max(g.count[e], 0), max(group_start(g, e + 1) - o, 0)) + 127) / 128;
+    }
+    p.out = static_cast<uint8_t *>(p.out) + static_cast<size_t>(e) * p.R * p.M * (OUT == 0 ? 2 : 4);
+    if (blocks == 0) {
+        if constexpr (OUT != 2) zero_tile<OUT>(p.out, p.M, ta * BA, min((ta + 1) * BA, p.M), tb * BB, min((tb + 1) * BB, p.R));
+        return;
+    }
+    lds_tile<WA, WB, GA, GB, 1, WIDE, OUT, false>(p, ta * BA, tb * BB, o / 128, o / 128 + blocks, 0);
+}
+
+// Most tiles of bb rows that the groups can make: each is a multiple of align rows, and their sum is within the rows.
+static long most_tiles(const GroupArgs &g, long pairs, int bb) {
+    const long rows = std::min<long>(g.rows, (pairs + std::min<long>(g.n, pairs) * (g.align - 1)) / g.align * g.align);
+    if (bb <= g.align) return rows / bb;
+    const long groups = std::min<long>(std::min<long>(g.n, pairs), rows / g.align);
+    return (rows + groups * (bb - g.align)) / bb;
+}
+
+template <int WA, int WB, int GA, int GB, bool WIDE, int OUT>
+static void tiled(const ProductArgs &p, const GroupArgs &g, long pairs, hipStream_t s) {
+    const int na = (p.M + 16 * WA * GA - 1) / (16 * WA * GA);
+    const long nb = most_tiles(g, pairs, 16 * WB * GB);
+    hipLaunchKernelGGL((expert_tiled<WA, WB, GA, GB, WIDE, OUT>), dim3(na * nb), dim3(64 * GA * GB), 0, s, p, g, na);
+}
+template <int RA, int TB, int W, bool WIDE, int OUT>
+static void direct(const ProductArgs &p, const GroupArgs &g, long pairs, hipStream_t s) {
+    const int na = (p.M + 16 * RA - 1) / (16 * RA);
+    const long nb = most_tiles(g, pairs, 16 * TB);
+    hipLaunchKernelGGL((expert_direct<RA, TB, W, WIDE, OUT>), dim3(na, nb), dim3(64 * W), 0, s, p, g);
+}
+
+template <bool WIDE, int OUT>
+static hipError_t product(const ProductArgs &p, const GroupArgs &g, long pairs, float mean, hipStream_t s) {
+    if (mean <= 16) direct<1, 1, 8, WIDE, OUT>(p, g, pairs, s);
+    else if (mean <= 48) tiled<4, 2, 2, 2, WIDE, OUT>(p, g, pairs, s);
+    else if (WIDE || mean <= 128) tiled<4, 4, 2, 2, WIDE, OUT>(p, g, pairs, s);
+    else if constexpr (!WIDE) tiled<8, 4, 2, 4, WIDE, OUT>(p, g, pairs, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_expert_product(const ProductArgs &p, const GroupArgs &g, long pairs, float mean, int out, hipStream_t s) {
+    return out == 0 ? product<false, 0>(p, g, pairs, mean, s) : product<true, 1>(p, g, pairs, mean, s);
+}
+
+template <int WA, int WB, int GA, int GB, bool WIDE, int OUT>
+static void grad(const ProductArgs &p, const GroupArgs &g, hipStream_t s) {
+    const int na = (p.M + 16 * WA * GA - 1) / (16 * WA * GA), nb = (p.R + 16 * WB * GB - 1) / (16 * WB * GB);
+    hipLaunchKernelGGL((expert_grad<WA, WB, GA, GB, WIDE, OUT>), dim3(g.n * na * nb), dim3(64 * GA * GB), 0, s, p, g, na, nb);
+}
+
+hipError_t launch_expert_weight_grad(const ProductArgs &p, const GroupArgs &g, int out, hipStream_t s) {
+    if (out == 0) grad<8, 4, 2, 4, false, 0>(p, g, s);
+    else if (out == 1) grad<4, 4, 2, 2, true, 1>(p, g, s);
+    else grad<4, 4, 2, 2, true, 2>(p, g, s);
+    return hipGetLastError();
+}
+
+}  // namespace ftmoe

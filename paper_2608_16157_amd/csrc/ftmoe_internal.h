@@ -81,6 +81,47 @@ struct BalanceArgs {
     float *d_logits;                  // [T][E]
 };
 
+// Pairs sorted by expert (sort.hip).
+struct SortArgs {
+    const int32_t *ids;     // [T][k]
+    const uint8_t *mask;    // [T] or null
+    int pairs, k, first, n, align, rows;
+    int32_t *row_pair, *pair_row, *off, *count, *dropped;
+    int chunk, blocks;      // pairs a workgroup places, workgroups
+    int32_t *table;         // [n][blocks] pairs of an expert in a workgroup's chunk, then in those before it
+    int32_t *totals;        // [n]
+};
+constexpr int kSortPairs = 4096;     // pairs that a workgroup holds at once
+constexpr int kSortMaxBlocks = 1024;
+
+// Rows in the order of the groups, and back (dispatch.hip).
+struct RowsArgs {
+    const int32_t *row_pair, *pair_row, *off;
+    const float *w;         // [T][k] or null
+    int T, k, n, rows, C;
+};
+
+// Groups of rows, one per expert, for a product (expert_products.hip).
+struct GroupArgs {
+    const int32_t *off, *count;
+    int n, align, rows;
+    size_t a_stride, as_stride;   // elements from one expert's weight, and scales, to the next
+};
+
+// Norms before and after a block (norm.hip).
+struct NormArgs {
+    const void *x, *b;          // forward: x, block output; backward: r, block output
+    const void *dr, *dn;        // backward
+    const void *pre, *post, *gate;   // [C] or null
+    const float *tgate;         // [T] or null
+    void *r, *nout;             // forward: outputs; backward: dx, db
+    ActForm row;                // forward: the row form of n
+    float *d_tgate;             // backward
+    float *parts;               // backward: [parts][2][C] column sums
+    int n_parts, T, C, post_norm;
+    float eps, scale;
+};
+
 struct HostMailbox;   // a worker pool's device <-> host mailbox (defined with CpuPool)
 
 // Routing outputs (the caller's ft_route_t, flattened).
@@ -398,7 +439,8 @@ hipError_t launch_swiglu_quantize(const void *gu, bool f32, int T, int I, const 
                                   hipStream_t s);
 hipError_t launch_swiglu_backward(const ActForm &saved, const void *dh, bool f32, int T, int I, const ActForm &drow,
                                   const ActForm &dcol, const ActForm &hcol, hipStream_t s);
-hipError_t launch_weight_transpose(const uint8_t *w, const float *s, uint8_t *wt, float *st, int N, int K, hipStream_t stream);
+// n weights, one behind the other
+hipError_t launch_weight_transpose(const uint8_t *w, const float *s, uint8_t *wt, float *st, int n, int N, int K, hipStream_t stream);
 // bx: 0 B is codes, 1 x is bf16, 2 x is float32 (only up to kDirectTokens rows); out: 0 bf16, 1 float32, 2 added
 // ws: room for the parts of a split reduction, or null
 hipError_t launch_product(const ProductArgs &p, bool a_e8m0, int bx, int out, float *ws, hipStream_t s);
@@ -413,5 +455,20 @@ constexpr int kBalMaxParts = 256;      // beyond: parts of the tokens, one workg
 constexpr int kBalMinPart = 32;
 hipError_t launch_balance(const BalanceArgs &a, hipStream_t s);
 hipError_t launch_router_backward(const BalanceArgs &a, hipStream_t s);
+
+hipError_t launch_sort(const SortArgs &a, hipStream_t s);
+// null codes, null plain rows: left out
+hipError_t launch_gather(const RowsArgs &a, const void *x, bool x_f32, void *plain, bool plain_f32, const ActForm &row,
+                         const ActForm &col, hipStream_t s);
+hipError_t launch_combine(const RowsArgs &a, const void *rows, bool rows_f32, const void *base, void *y, bool y_f32, hipStream_t s);
+hipError_t launch_gate_grad(const RowsArgs &a, const void *rows, bool rows_f32, const void *dy, bool dy_f32, float *d_w, hipStream_t s);
+// pairs: the most that the groups can hold, mean: expected in one of them; out as for launch_product
+hipError_t launch_expert_product(const ProductArgs &p, const GroupArgs &g, long pairs, float mean, int out, hipStream_t s);
+hipError_t launch_expert_weight_grad(const ProductArgs &p, const GroupArgs &g, int out, hipStream_t s);
+// parts of the column sums that a backward pass leaves (NormArgs.n_parts)
+int norm_parts(int T, int C);
+hipError_t launch_block_norm(const NormArgs &a, bool x_f32, bool y_f32, bool w_f32, hipStream_t s);
+hipError_t launch_block_norm_backward(const NormArgs &a, bool x_f32, bool y_f32, bool w_f32, float *d_pre, float *d_post,
+                                      float *d_gate, hipStream_t s);
 
 }  // namespace ftmoe

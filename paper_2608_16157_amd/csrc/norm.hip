@@ -1,0 +1,364 @@
+// Norms before and after a block, fused with the block's gates and residual scale (ft_block_norm), and their
+// backward pass.  With 1/rms(v) = (mean v^2 + eps)^-1/2, g the gate per channel, h the gate per token:
+//
+//   u = post b / rms(b)  (or b),   r = x + scale g h u,   n = pre r / rms(r)
+//
+// Backward, from r, b and the gradients dr, dn of r and n; G = dn pre, sums over the channels of a token:
+//   d  = dr + (G - r mean(G r) / rms(r)^2) / rms(r)                   gradient of x
+//   S  = sum scale g d post b                                         dh = S / rms(b)
+//   db = (scale g h post d - b (h S / C) / rms(b)^2) / rms(b)         (scale g h d without a norm after the block)
+//   and over the tokens  A = sum h d b / rms(b),  B = sum dn r / rms(r):
+//   d_post = scale g A,  d_gate = scale post A,  d_pre = B
+//
+// A row lies in the registers of its LANES threads (8 CH channels a thread, LANES x 8 channels a step), so each matrix
+// is read once.  Row sums: lanes of a wave, then the waves in order through LDS.  Column sums: a thread's own over the rows
+// of its workgroup, then over the workgroups in order, in float64.
+//
+// The bound is HBM.
+#include "act_codes.h"
+#include "ftmoe_internal.h"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace ftmoe {
+
+template <class T>
+__device__ __forceinline__ void put8(T *p, const float *v) {
+    if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<uint4 *>(p) =
+            uint4{f32_to_bf16_any(v[0]) | f32_to_bf16_any(v[1]) << 16, f32_to_bf16_any(v[2]) | f32_to_bf16_any(v[3]) << 16,
+                  f32_to_bf16_any(v[4]) | f32_to_bf16_any(v[5]) << 16, f32_to_bf16_any(v[6]) | f32_to_bf16_any(v[7]) << 16};
+    } else {
+        reinterpret_cast<float4 *>(p)[0] = float4{v[0], v[1], v[2], v[3]};
+        reinterpret_cast<float4 *>(p)[1] = float4{v[4], v[5], v[6], v[7]};
+    }
+}
+
+// 8 channels of a weight or gate; ones where there is none
+__device__ __forceinline__ void channels8(const void *w, bool f32, int c, float *v) {
+    if (!w) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = 1.0f;
+    } else if (f32) {
+        load8(static_cast<const float *>(w) + c, v);
+    } else {
+        load8(static_cast<const uint16_t *>(w) + c, v);
+    }
+}
+
+// Sums of N values over the threads of a row, in every one of them.  `turn` alternates between two buffers: whoever
+// writes one again has passed the barrier behind the last reading of it.
+template <int LANES, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float (*buf)[16][N], int &turn) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = wave_sum_f32(v[i]);
+    if constexpr (LANES > 64) {
+        const int wave = threadIdx.x / 64;
+        if (lane_id() == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) buf[turn][wave][i] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < LANES / 64; ++w)
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] += buf[turn][w][i];
+        turn ^= 1;
+    }
+}
+
+__device__ __forceinline__ float over_rms(float sum, const NormArgs &a) { return 1.0f / sqrtf(sum / a.C + a.eps); }
+
+template <class XT, class YT, int LANES, int CH>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void block_norm(NormArgs a, bool w_f32) {
+    constexpr int kRows = LANES < 256 ? 256 / LANES : 1;   // rows of a workgroup at once
+    constexpr bool kHold = CH <= 2;                        // weights stay in registers
+    __shared__ float buf[2][16][1];
+    int turn = 0;
+    const int lane = threadIdx.x % LANES;
+    int c[CH];
+    bool in[CH];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        c[i] = (i * LANES + lane) * 8;
+        in[i] = c[i] < a.C;
+    }
+    float pre[kHold ? CH : 1][8], up[kHold ? CH : 1][8];   // up: scale gate post
+    auto weights = [&](int i, float *wp, float *wu) {
+        float g[8];
+        const int at = min(c[i], a.C - 8);
+        channels8(a.pre, w_f32, at, wp);
+        channels8(a.post_norm ? a.post : nullptr, w_f32, at, wu);
+        channels8(a.gate, w_f32, at, g);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) wu[q] *= a.scale * g[q];
+    };
+    if constexpr (kHold)
+#pragma unroll
+        for (int i = 0; i < CH; ++i) weights(i, pre[i], up[i]);
+    for (long row = static_cast<long>(blockIdx.x) * kRows + threadIdx.x / LANES; row < a.T; row += static_cast<long>(gridDim.x) * kRows) {
+        const size_t at = static_cast<size_t>(row) * a.C;
+        float x[CH][8], b[CH][8];
+#pragma unroll
+        for (int i = 0; i < CH; ++i) load8(static_cast<const XT *>(a.x) + at + min(c[i], a.C - 8), x[i]);
+        if (a.b) {
+#pragma unroll
+            for (int i = 0; i < CH; ++i) load8(static_cast<const YT *>(a.b) + at + min(c[i], a.C - 8), b[i]);
+            float h = a.tgate ? a.tgate[row] : 1.0f;
+            if (a.post_norm) {
+                float s[1] = {0.0f};
+#pragma unroll
+                for (int i = 0; i < CH; ++i)
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) s[0] = fmaf(in[i] ? b[i][q] : 0.0f, b[i][q], s[0]);
+                row_sums<LANES, 1>(s, buf, turn);
+                h *= over_rms(s[0], a);
+            }
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                float wp[8], wu[8];
+                if constexpr (!kHold) weights(i, wp, wu);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) x[i][q] = fmaf(kHold ? up[kHold ? i : 0][q] : wu[q], b[i][q] * h, x[i][q]);
+                if (in[i] && a.r) put8(static_cast<XT *>(a.r) + at + c[i], x[i]);
+            }
+        }
+        if (!a.nout && !a.row.codes) continue;
+        float s[1] = {0.0f};
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) s[0] = fmaf(in[i] ? x[i][q] : 0.0f, x[i][q], s[0]);
+        row_sums<LANES, 1>(s, buf, turn);
+        const float rr = over_rms(s[0], a);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            float wp[8], wu[8], n[8];
+            if constexpr (!kHold) weights(i, wp, wu);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) n[q] = in[i] ? x[i][q] * rr * (kHold ? pre[kHold ? i : 0][q] : wp[q]) : 0.0f;
+            if (in[i] && a.nout) put8(static_cast<YT *>(a.nout) + at + c[i], n);
+            if (a.row.codes && c[i] < a.row.Kp) {   // Kp is a multiple of 128: whole lane rows of 16
+                const int byte = act_scale_byte(block_mag16(n));
+                const float sc = act_scale_operand(byte);
+                *reinterpret_cast<uint2 *>(a.row.codes + static_cast<size_t>(row) * a.row.Kp + c[i]) =
+                    uint2{act_codes4(n[0], n[1], n[2], n[3], sc), act_codes4(n[4], n[5], n[6], n[7], sc)};
+                if (lane % 16 == 0) a.row.scales[static_cast<size_t>(c[i] / 128) * a.row.Rp + row] = static_cast<uint8_t>(byte);
+            }
+        }
+    }
+    // scales of the rows that fill the form up
+    if (a.row.codes && blockIdx.x == 0) {
+        const int more = a.row.Rp - a.T;
+        for (int i = threadIdx.x; i < more * (a.row.Kp / 128); i += blockDim.x)
+            a.row.scales[static_cast<size_t>(i / more) * a.row.Rp + a.T + i % more] = 127;
+    }
+}
+
+template <class XT, class YT, int LANES, int CH>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void block_norm_backward(NormArgs a, bool w_f32) {
+    constexpr int kRows = LANES < 256 ? 256 / LANES : 1;
+    constexpr bool kHold = CH <= 2;
+    __shared__ float buf3[2][16][3], buf1[2][16][1];
+    int turn3 = 0, turn1 = 0;
+    const int lane = threadIdx.x % LANES;
+    int c[CH];
+    bool in[CH];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        c[i] = (i * LANES + lane) * 8;
+        in[i] = c[i] < a.C;
+    }
+    float pre[kHold ? CH : 1][8], up[kHold ? CH : 1][8];
+    auto weights = [&](int i, float *wp, float *wu) {
+        float g[8];
+        const int at = min(c[i], a.C - 8);
+        channels8(a.pre, w_f32, at, wp);
+        channels8(a.post_norm ? a.post : nullptr, w_f32, at, wu);
+        channels8(a.gate, w_f32, at, g);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) wu[q] *= a.scale * g[q];
+    };
+    if constexpr (kHold)
+#pragma unroll
+        for (int i = 0; i < CH; ++i) weights(i, pre[i], up[i]);
+    float sa[CH][8], sb[CH][8];   // A and B over this workgroup's rows
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) sa[i][q] = sb[i][q] = 0.0f;
+    const long part = static_cast<long>(blockIdx.x) * kRows + threadIdx.x / LANES;
+    for (long row = part; row < a.T; row += static_cast<long>(gridDim.x) * kRows) {
+        const size_t at = static_cast<size_t>(row) * a.C;
+        float r[CH][8], b[CH][8], d[CH][8], dn[CH][8];
+#pragma unroll
+        for (int i = 0; i < CH; ++i) load8(static_cast<const XT *>(a.x) + at + min(c[i], a.C - 8), r[i]);
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) d[i][q] = dn[i][q] = b[i][q] = 0.0f;
+        if (a.dn)
+#pragma unroll
+            for (int i = 0; i < CH; ++i) load8(static_cast<const YT *>(a.dn) + at + min(c[i], a.C - 8), dn[i]);
+        if (a.b)
+#pragma unroll
+            for (int i = 0; i < CH; ++i) load8(static_cast<const YT *>(a.b) + at + min(c[i], a.C - 8), b[i]);
+        if (a.dr)
+#pragma unroll
+            for (int i = 0; i < CH; ++i) load8(static_cast<const XT *>(a.dr) + at + min(c[i], a.C - 8), d[i]);
+        float s[3] = {0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            float wp[8], wu[8];
+            if constexpr (!kHold) weights(i, wp, wu);
+            if (in[i])
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    s[0] = fmaf(r[i][q], r[i][q], s[0]);
+                    s[1] = fmaf(dn[i][q] * (kHold ? pre[kHold ? i : 0][q] : wp[q]), r[i][q], s[1]);
+                    s[2] = fmaf(b[i][q], b[i][q], s[2]);
+                }
+        }
+        row_sums<LANES, 3>(s, buf3, turn3);
+        const float rr = over_rms(s[0], a), rb = a.post_norm ? over_rms(s[2], a) : 1.0f;
+        const float mean = s[1] / a.C * rr * rr;
+        const float h = a.tgate ? a.tgate[row] : 1.0f;
+        float t[1] = {0.0f};
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            float wp[8], wu[8];
+            if constexpr (!kHold) weights(i, wp, wu);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const float g = dn[i][q] * (kHold ? pre[kHold ? i : 0][q] : wp[q]);
+                if (a.dn) d[i][q] = fmaf(rr, fmaf(-mean, r[i][q], g), d[i][q]);
+                sb[i][q] = fmaf(dn[i][q], r[i][q] * rr, sb[i][q]);
+                sa[i][q] = fmaf(h * rb * d[i][q], b[i][q], sa[i][q]);
+                const float v = (kHold ? up[kHold ? i : 0][q] : wu[q]) * d[i][q];
+                if (in[i]) t[0] = fmaf(v, b[i][q], t[0]);
+            }
+            if (in[i] && a.r) put8(static_cast<XT *>(a.r) + at + c[i], d[i]);
+        }
+        if (!a.b) continue;
+        if (a.post_norm || a.d_tgate) row_sums<LANES, 1>(t, buf1, turn1);
+        if (a.d_tgate && lane == 0) a.d_tgate[row] = t[0] * rb;
+        const float off = a.post_norm ? t[0] / a.C * rb * rb : 0.0f;
+        if (!a.nout) continue;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            float wp[8], wu[8], o[8];
+            if constexpr (!kHold) weights(i, wp, wu);
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                o[q] = h * rb * fmaf(-off, b[i][q], (kHold ? up[kHold ? i : 0][q] : wu[q]) * d[i][q]);
+            if (in[i]) put8(static_cast<YT *>(a.nout) + at + c[i], o);
+        }
+    }
+    if (!a.parts) return;
+    float *mine = a.parts + static_cast<size_t>(part) * 2 * a.C;
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+        if (in[i]) {
+            put8(mine + c[i], sa[i]);
+            put8(mine + a.C + c[i], sb[i]);
+        }
+}
+
+// Column sums of the parts: 64 columns of A or B per workgroup, 16 runs of parts by 16 threads of 4 columns.
+__global__ __launch_bounds__(256) void block_norm_join(NormArgs a, bool w_f32, float *d_pre, float *d_post, float *d_gate) {
+    __shared__ double sums[16][64];
+    const int run = threadIdx.x / 16, col = blockIdx.x * 64 + 4 * (threadIdx.x % 16);
+    const bool second = blockIdx.y == 1;
+    double v[4] = {0.0, 0.0, 0.0, 0.0};
+    if (col < a.C) {
+        const float *p = a.parts + (second ? a.C : 0) + col;
+#pragma unroll 8
+        for (int i = run; i < a.n_parts; i += 16) {
+            const float4 f = *reinterpret_cast<const float4 *>(p + static_cast<size_t>(i) * 2 * a.C);
+            v[0] += f.x;
+            v[1] += f.y;
+            v[2] += f.z;
+            v[3] += f.w;
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sums[run][4 * (threadIdx.x % 16) + q] = v[q];
+    __syncthreads();
+    const int c = blockIdx.x * 64 + threadIdx.x;
+    if (threadIdx.x >= 64 || c >= a.C) return;
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s += sums[i][threadIdx.x];
+    if (second) {
+        if (d_pre) d_pre[c] = static_cast<float>(s);
+        return;
+    }
+    auto at = [&](const void *w) {
+        if (!w) return 1.0f;
+        return w_f32 ? static_cast<const float *>(w)[c] : __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t *>(w)[c]) << 16);
+    };
+    if (d_post) d_post[c] = static_cast<float>(s * a.scale * at(a.gate));
+    if (d_gate) d_gate[c] = static_cast<float>(s * a.scale * at(a.post_norm ? a.post : nullptr));
+}
+
+// Threads of a row, and rows of a workgroup, by the channels.
+struct NormShape {
+    int lanes, rows;
+};
+static NormShape norm_shape(int C) {
+    if (C <= 1024) return {64, 4};
+    if (C <= 4096) return {256, 1};
+    return {1024, 1};
+}
+// Workgroups: as many as run at once, so that each holds its weights for several rows and leaves one part.
+static int norm_blocks(int T, int C) {
+    const NormShape n = norm_shape(C);
+    return std::min((T + n.rows - 1) / n.rows, n.lanes == 1024 ? 512 : 1024);
+}
+int norm_parts(int T, int C) { return norm_blocks(T, C) * norm_shape(C).rows; }
+
+template <class XT, class YT, bool BACK>
+static void norm_go(const NormArgs &a, bool w_f32, hipStream_t s) {
+    const dim3 grid(norm_blocks(a.T, a.C));
+    auto go = [&](auto lanes, auto chunks) {
+        constexpr int L = decltype(lanes)::value, CH = decltype(chunks)::value;
+        if constexpr (BACK) hipLaunchKernelGGL((block_norm_backward<XT, YT, L, CH>), grid, dim3(std::max(L, 256)), 0, s, a, w_f32);
+        else hipLaunchKernelGGL((block_norm<XT, YT, L, CH>), grid, dim3(std::max(L, 256)), 0, s, a, w_f32);
+    };
+    std::integral_constant<int, 64> l64;
+    std::integral_constant<int, 256> l256;
+    std::integral_constant<int, 1024> l1024;
+    std::integral_constant<int, 1> c1;
+    std::integral_constant<int, 2> c2;
+    std::integral_constant<int, 8> c8;
+    if (a.C <= 512) go(l64, c1);
+    else if (a.C <= 1024) go(l64, c2);
+    else if (a.C <= 2048) go(l256, c1);
+    else if (a.C <= 4096) go(l256, c2);
+    else if (a.C <= 8192) go(l1024, c1);
+    else if (a.C <= 16384) go(l1024, c2);
+    else go(l1024, c8);
+}
+
+template <bool BACK>
+static void norm_types(const NormArgs &a, bool x_f32, bool y_f32, bool w_f32, hipStream_t s) {
+    if (x_f32) y_f32 ? norm_go<float, float, BACK>(a, w_f32, s) : norm_go<float, uint16_t, BACK>(a, w_f32, s);
+    else y_f32 ? norm_go<uint16_t, float, BACK>(a, w_f32, s) : norm_go<uint16_t, uint16_t, BACK>(a, w_f32, s);
+}
+
+hipError_t launch_block_norm(const NormArgs &a, bool x_f32, bool y_f32, bool w_f32, hipStream_t s) {
+    norm_types<false>(a, x_f32, y_f32, w_f32, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_block_norm_backward(const NormArgs &a, bool x_f32, bool y_f32, bool w_f32, float *d_pre, float *d_post,
+                                      float *d_gate, hipStream_t s) {
+    if (a.T > 0) norm_types<true>(a, x_f32, y_f32, w_f32, s);
+    if (a.parts)
+        hipLaunchKernelGGL(block_norm_join, dim3((a.C + 63) / 64, 2), dim3(256), 0, s, a, w_f32, d_pre, d_post, d_gate);
+    return hipGetLastError();
+}
+
+}  // namespace ftmoe
