@@ -46,6 +46,18 @@ __device__ __forceinline__ void zero_unless(bool in, float (&v)[N]) {
 #pragma unroll
         for (int q = 0; q < N; ++q) v[q] = 0.0f;
 }
+// eight values out, rounded to nearest even where they are bf16 (one instruction for two; a NaN stays one)
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(a), static_cast<__bf16>(b)});
+}
+__device__ __forceinline__ void store8(uint16_t *p, const float *v) {
+    *reinterpret_cast<uint4 *>(p) = uint4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
+}
+__device__ __forceinline__ void store8(float *p, const float *v) {
+    reinterpret_cast<float4 *>(p)[0] = float4{v[0], v[1], v[2], v[3]};
+    reinterpret_cast<float4 *>(p)[1] = float4{v[4], v[5], v[6], v[7]};
+}
 template <class XT>
 __device__ __forceinline__ void load16(const XT *p, float (&v)[16]) {
     load8(p, v);

@@ -4,6 +4,7 @@
 //
 // All of these move memory once and compute little: the bound is HBM.
 #include "act_tile.h"
+#include "gemm_tile.h"
 
 namespace ftmoe {
 
@@ -17,19 +18,6 @@ __device__ __forceinline__ int row_token(const RowsArgs &a, long row, float &w) 
 }
 // one past the last group's rows
 __device__ __forceinline__ int rows_end(const RowsArgs &a) { return min(a.off[a.n], a.rows); }
-
-__device__ __forceinline__ void store8(uint16_t *p, const float *v) {
-    uint4 o;
-    o.x = f32_to_bf16_any(v[0]) | f32_to_bf16_any(v[1]) << 16;
-    o.y = f32_to_bf16_any(v[2]) | f32_to_bf16_any(v[3]) << 16;
-    o.z = f32_to_bf16_any(v[4]) | f32_to_bf16_any(v[5]) << 16;
-    o.w = f32_to_bf16_any(v[6]) | f32_to_bf16_any(v[7]) << 16;
-    *reinterpret_cast<uint4 *>(p) = o;
-}
-__device__ __forceinline__ void store8(float *p, const float *v) {
-    reinterpret_cast<float4 *>(p)[0] = float4{v[0], v[1], v[2], v[3]};
-    reinterpret_cast<float4 *>(p)[1] = float4{v[4], v[5], v[6], v[7]};
-}
 
 // Plain rows: one wave per row.
 template <class XT, class OT>
@@ -80,8 +68,10 @@ template <class XT>
 __global__ __launch_bounds__(kActThreads) void gather_tiles(RowsArgs a, const XT *x, ActForm row, ActForm col) {
     __shared__ __attribute__((aligned(16))) ActTileShared<1> sh;
     const int g = threadIdx.x / 16, sub = threadIdx.x % 16;
-    const int cb = blockIdx.x, rb = blockIdx.y, row0 = rb * 128 + kActRows * g, c = cb * 128 + 8 * sub;
-    if (rb * 128 >= rows_end(a)) return;
+    const int nkb = (a.C + 127) / 128, nrb = rows_end(a) / 128;
+    if (static_cast<int>(blockIdx.x) >= nkb * nrb) return;
+    const int L = xcd_remap(blockIdx.x, nkb * nrb), cb = L / nrb, rb = L - cb * nrb;
+    const int row0 = rb * 128 + kActRows * g, c = cb * 128 + 8 * sub;
     float v[1][kActRows][8], w[kActRows];
     int t[kActRows];
 #pragma unroll
@@ -112,7 +102,7 @@ static void gather(const RowsArgs &a, const XT *x, void *plain, bool plain_f32, 
     }
     const unsigned nkb = (a.C + 127) / 128;
     if (col.codes)
-        hipLaunchKernelGGL(gather_tiles<XT>, dim3(nkb, a.rows / 128), dim3(kActThreads), 0, s, a, x, row, col);
+        hipLaunchKernelGGL(gather_tiles<XT>, dim3(nkb * (a.rows / 128)), dim3(kActThreads), 0, s, a, x, row, col);
     else if (row.codes)
         hipLaunchKernelGGL(gather_rows<XT>, dim3(nkb, (a.rows + 63) / 64), dim3(256), 0, s, a, x, row);
 }

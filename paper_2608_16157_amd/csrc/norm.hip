@@ -15,25 +15,13 @@
 // of its workgroup, then over the workgroups in order, in float64.
 //
 // The bound is HBM.
-#include "act_codes.h"
-#include "ftmoe_internal.h"
+#include "act_tile.h"
 
 #include <algorithm>
 #include <type_traits>
 
 namespace ftmoe {
 
-template <class T>
-__device__ __forceinline__ void put8(T *p, const float *v) {
-    if constexpr (sizeof(T) == 2) {
-        *reinterpret_cast<uint4 *>(p) =
-            uint4{f32_to_bf16_any(v[0]) | f32_to_bf16_any(v[1]) << 16, f32_to_bf16_any(v[2]) | f32_to_bf16_any(v[3]) << 16,
-                  f32_to_bf16_any(v[4]) | f32_to_bf16_any(v[5]) << 16, f32_to_bf16_any(v[6]) | f32_to_bf16_any(v[7]) << 16};
-    } else {
-        reinterpret_cast<float4 *>(p)[0] = float4{v[0], v[1], v[2], v[3]};
-        reinterpret_cast<float4 *>(p)[1] = float4{v[4], v[5], v[6], v[7]};
-    }
-}
 
 // 8 channels of a weight or gate; ones where there is none
 __device__ __forceinline__ void channels8(const void *w, bool f32, int c, float *v) {
@@ -50,21 +38,25 @@ __device__ __forceinline__ void channels8(const void *w, bool f32, int c, float 
 // Sums of N values over the threads of a row, in every one of them.  `turn` alternates between two buffers: whoever
 // writes one again has passed the barrier behind the last reading of it.
 template <int LANES, int N>
-__device__ __forceinline__ void row_sums(float (&v)[N], float (*buf)[16][N], int &turn) {
+__device__ __forceinline__ void row_sums(float (&v)[N], float (*buf)[N][16], int &turn) {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = wave_sum_f32(v[i]);
     if constexpr (LANES > 64) {
-        const int wave = threadIdx.x / 64;
+        constexpr int kWaves = LANES / 64;
         if (lane_id() == 0)
 #pragma unroll
-            for (int i = 0; i < N; ++i) buf[turn][wave][i] = v[i];
+            for (int i = 0; i < N; ++i) buf[turn][i][threadIdx.x / 64] = v[i];
         __syncthreads();
+        // every lane row of 16 adds up the waves' sums for itself
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = 0.0f;
-#pragma unroll
-        for (int w = 0; w < LANES / 64; ++w)
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] += buf[turn][w][i];
+        for (int i = 0; i < N; ++i) {
+            const float p = buf[turn][i][lane_id() % kWaves];
+            v[i] = lane_id() % 16 < kWaves ? p : 0.0f;
+            v[i] += __uint_as_float(dpp_u32<kDppRowRor1>(__float_as_uint(v[i])));
+            v[i] += __uint_as_float(dpp_u32<kDppRowRor2>(__float_as_uint(v[i])));
+            v[i] += __uint_as_float(dpp_u32<kDppRowRor4>(__float_as_uint(v[i])));
+            v[i] += __uint_as_float(dpp_u32<kDppRowRor8>(__float_as_uint(v[i])));
+        }
         turn ^= 1;
     }
 }
@@ -75,7 +67,7 @@ template <class XT, class YT, int LANES, int CH>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void block_norm(NormArgs a, bool w_f32) {
     constexpr int kRows = LANES < 256 ? 256 / LANES : 1;   // rows of a workgroup at once
     constexpr bool kHold = CH <= 2;                        // weights stay in registers
-    __shared__ float buf[2][16][1];
+    __shared__ float buf[2][1][16];
     int turn = 0;
     const int lane = threadIdx.x % LANES;
     int c[CH];
@@ -122,7 +114,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void block_norm(NormArgs
                 if constexpr (!kHold) weights(i, wp, wu);
 #pragma unroll
                 for (int q = 0; q < 8; ++q) x[i][q] = fmaf(kHold ? up[kHold ? i : 0][q] : wu[q], b[i][q] * h, x[i][q]);
-                if (in[i] && a.r) put8(static_cast<XT *>(a.r) + at + c[i], x[i]);
+                if (in[i] && a.r) store8(static_cast<XT *>(a.r) + at + c[i], x[i]);
             }
         }
         if (!a.nout && !a.row.codes) continue;
@@ -139,7 +131,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void block_norm(NormArgs
             if constexpr (!kHold) weights(i, wp, wu);
 #pragma unroll
             for (int q = 0; q < 8; ++q) n[q] = in[i] ? x[i][q] * rr * (kHold ? pre[kHold ? i : 0][q] : wp[q]) : 0.0f;
-            if (in[i] && a.nout) put8(static_cast<YT *>(a.nout) + at + c[i], n);
+            if (in[i] && a.nout) store8(static_cast<YT *>(a.nout) + at + c[i], n);
             if (a.row.codes && c[i] < a.row.Kp) {   // Kp is a multiple of 128: whole lane rows of 16
                 const int byte = act_scale_byte(block_mag16(n));
                 const float sc = act_scale_operand(byte);
@@ -157,11 +149,39 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void block_norm(NormArgs
     }
 }
 
+// 8 channels as they lie in memory, and their values
+template <class T>
+struct Raw8 {
+    uint4 w[sizeof(T) / 2];
+};
+template <class T>
+__device__ __forceinline__ void fetch8(const void *p, size_t at, Raw8<T> &r) {
+    const uint4 *q = reinterpret_cast<const uint4 *>(static_cast<const T *>(p) + at);
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) r.w[i] = q[i];
+}
+template <class T>
+__device__ __forceinline__ void values8(const Raw8<T> &r, float *v) {
+    uint32_t w[2 * sizeof(T)];
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) {
+        w[4 * i] = r.w[i].x;
+        w[4 * i + 1] = r.w[i].y;
+        w[4 * i + 2] = r.w[i].z;
+        w[4 * i + 3] = r.w[i].w;
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+        v[q] = __uint_as_float(sizeof(T) == 4 ? w[q] : q % 2 ? w[q / 2] & 0xFFFF0000u : w[q / 2] << 16);
+}
+
+// A row's channels of a thread; the next row's are requested before the sums of this one are waited for: a workgroup
+// of 1024 threads fills a CU.  Up to 8192 channels nothing spills.
 template <class XT, class YT, int LANES, int CH>
-__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void block_norm_backward(NormArgs a, bool w_f32) {
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES == 1024 ? 4 : 3) void block_norm_backward(NormArgs a, bool w_f32) {
     constexpr int kRows = LANES < 256 ? 256 / LANES : 1;
     constexpr bool kHold = CH <= 2;
-    __shared__ float buf3[2][16][3], buf1[2][16][1];
+    __shared__ float buf3[2][3][16], buf1[2][1][16];
     int turn3 = 0, turn1 = 0;
     const int lane = threadIdx.x % LANES;
     int c[CH];
@@ -189,26 +209,39 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void block_norm_backward
     for (int i = 0; i < CH; ++i)
 #pragma unroll
         for (int q = 0; q < 8; ++q) sa[i][q] = sb[i][q] = 0.0f;
-    const long part = static_cast<long>(blockIdx.x) * kRows + threadIdx.x / LANES;
-    for (long row = part; row < a.T; row += static_cast<long>(gridDim.x) * kRows) {
+    const long part = static_cast<long>(blockIdx.x) * kRows + threadIdx.x / LANES, stride = static_cast<long>(gridDim.x) * kRows;
+    Raw8<XT> r8[CH], d8[CH] = {};
+    Raw8<YT> b8[CH] = {}, n8[CH] = {};
+    float h8 = 1.0f;
+    auto request = [&](long row) {   // of rows past the last one: the last one, unused
+        row = min(row, a.T - 1L);
         const size_t at = static_cast<size_t>(row) * a.C;
-        float r[CH][8], b[CH][8], d[CH][8], dn[CH][8];
 #pragma unroll
-        for (int i = 0; i < CH; ++i) load8(static_cast<const XT *>(a.x) + at + min(c[i], a.C - 8), r[i]);
-#pragma unroll
-        for (int i = 0; i < CH; ++i)
-#pragma unroll
-            for (int q = 0; q < 8; ++q) d[i][q] = dn[i][q] = b[i][q] = 0.0f;
+        for (int i = 0; i < CH; ++i) fetch8<XT>(a.x, at + min(c[i], a.C - 8), r8[i]);
         if (a.dn)
 #pragma unroll
-            for (int i = 0; i < CH; ++i) load8(static_cast<const YT *>(a.dn) + at + min(c[i], a.C - 8), dn[i]);
+            for (int i = 0; i < CH; ++i) fetch8<YT>(a.dn, at + min(c[i], a.C - 8), n8[i]);
         if (a.b)
 #pragma unroll
-            for (int i = 0; i < CH; ++i) load8(static_cast<const YT *>(a.b) + at + min(c[i], a.C - 8), b[i]);
+            for (int i = 0; i < CH; ++i) fetch8<YT>(a.b, at + min(c[i], a.C - 8), b8[i]);
         if (a.dr)
 #pragma unroll
-            for (int i = 0; i < CH; ++i) load8(static_cast<const XT *>(a.dr) + at + min(c[i], a.C - 8), d[i]);
-        float s[3] = {0.0f, 0.0f, 0.0f};
+            for (int i = 0; i < CH; ++i) fetch8<XT>(a.dr, at + min(c[i], a.C - 8), d8[i]);
+        if (a.tgate) h8 = a.tgate[row];
+    };
+    request(part);
+    for (long row = part; row < a.T; row += stride) {
+        const size_t at = static_cast<size_t>(row) * a.C;
+        float r[CH][8], n[CH][8], b[CH][8], d[CH][8], s[3] = {0.0f, 0.0f, 0.0f};
+        const float h = h8;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            values8(r8[i], r[i]);
+            values8(n8[i], n[i]);
+            values8(b8[i], b[i]);
+            values8(d8[i], d[i]);
+        }
+        request(row + stride);
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             float wp[8], wu[8];
@@ -217,14 +250,13 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void block_norm_backward
 #pragma unroll
                 for (int q = 0; q < 8; ++q) {
                     s[0] = fmaf(r[i][q], r[i][q], s[0]);
-                    s[1] = fmaf(dn[i][q] * (kHold ? pre[kHold ? i : 0][q] : wp[q]), r[i][q], s[1]);
+                    s[1] = fmaf(n[i][q] * (kHold ? pre[kHold ? i : 0][q] : wp[q]), r[i][q], s[1]);
                     s[2] = fmaf(b[i][q], b[i][q], s[2]);
                 }
         }
         row_sums<LANES, 3>(s, buf3, turn3);
         const float rr = over_rms(s[0], a), rb = a.post_norm ? over_rms(s[2], a) : 1.0f;
-        const float mean = s[1] / a.C * rr * rr;
-        const float h = a.tgate ? a.tgate[row] : 1.0f;
+        const float mean = s[1] / a.C * rr * rr, hb = h * rb;
         float t[1] = {0.0f};
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
@@ -232,14 +264,17 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void block_norm_backward
             if constexpr (!kHold) weights(i, wp, wu);
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
-                const float g = dn[i][q] * (kHold ? pre[kHold ? i : 0][q] : wp[q]);
+                const float g = n[i][q] * (kHold ? pre[kHold ? i : 0][q] : wp[q]);
                 if (a.dn) d[i][q] = fmaf(rr, fmaf(-mean, r[i][q], g), d[i][q]);
-                sb[i][q] = fmaf(dn[i][q], r[i][q] * rr, sb[i][q]);
-                sa[i][q] = fmaf(h * rb * d[i][q], b[i][q], sa[i][q]);
-                const float v = (kHold ? up[kHold ? i : 0][q] : wu[q]) * d[i][q];
-                if (in[i]) t[0] = fmaf(v, b[i][q], t[0]);
+                sb[i][q] = fmaf(n[i][q], r[i][q] * rr, sb[i][q]);
+                sa[i][q] = fmaf(hb * d[i][q], b[i][q], sa[i][q]);
             }
-            if (in[i] && a.r) put8(static_cast<XT *>(a.r) + at + c[i], d[i]);
+            if (in[i] && a.r) store8(static_cast<XT *>(a.r) + at + c[i], d[i]);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                d[i][q] *= kHold ? up[kHold ? i : 0][q] : wu[q];   // scale gate post d
+                if (in[i]) t[0] = fmaf(d[i][q], b[i][q], t[0]);
+            }
         }
         if (!a.b) continue;
         if (a.post_norm || a.d_tgate) row_sums<LANES, 1>(t, buf1, turn1);
@@ -248,12 +283,9 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void block_norm_backward
         if (!a.nout) continue;
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            float wp[8], wu[8], o[8];
-            if constexpr (!kHold) weights(i, wp, wu);
 #pragma unroll
-            for (int q = 0; q < 8; ++q)
-                o[q] = h * rb * fmaf(-off, b[i][q], (kHold ? up[kHold ? i : 0][q] : wu[q]) * d[i][q]);
-            if (in[i]) put8(static_cast<YT *>(a.nout) + at + c[i], o);
+            for (int q = 0; q < 8; ++q) d[i][q] = hb * fmaf(-off, b[i][q], d[i][q]);
+            if (in[i]) store8(static_cast<YT *>(a.nout) + at + c[i], d[i]);
         }
     }
     if (!a.parts) return;
@@ -261,8 +293,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void block_norm_backward
 #pragma unroll
     for (int i = 0; i < CH; ++i)
         if (in[i]) {
-            put8(mine + c[i], sa[i]);
-            put8(mine + a.C + c[i], sb[i]);
+            store8(mine + c[i], sa[i]);
+            store8(mine + a.C + c[i], sb[i]);
         }
 }
 
@@ -308,20 +340,20 @@ struct NormShape {
     int lanes, rows;
 };
 static NormShape norm_shape(int C) {
-    if (C <= 1024) return {64, 4};
-    if (C <= 4096) return {256, 1};
-    return {1024, 1};
+    if (C <= 512) return {64, 4};
+    if (C <= 2048) return {256, 1};
+    return {C <= 4096 ? 512 : 1024, 1};
 }
 // Workgroups: as many as run at once, so that each holds its weights for several rows and leaves one part.
-static int norm_blocks(int T, int C) {
+static int norm_blocks(int T, int C, bool back) {
     const NormShape n = norm_shape(C);
-    return std::min((T + n.rows - 1) / n.rows, n.lanes == 1024 ? 512 : 1024);
+    return std::min((T + n.rows - 1) / n.rows, back ? 256 * 1024 / std::max(n.lanes, 256) : 512 * 1024 / std::max(n.lanes, 256));
 }
-int norm_parts(int T, int C) { return norm_blocks(T, C) * norm_shape(C).rows; }
+int norm_parts(int T, int C) { return norm_blocks(T, C, true) * norm_shape(C).rows; }
 
 template <class XT, class YT, bool BACK>
 static void norm_go(const NormArgs &a, bool w_f32, hipStream_t s) {
-    const dim3 grid(norm_blocks(a.T, a.C));
+    const dim3 grid(norm_blocks(a.T, a.C, BACK));
     auto go = [&](auto lanes, auto chunks) {
         constexpr int L = decltype(lanes)::value, CH = decltype(chunks)::value;
         if constexpr (BACK) hipLaunchKernelGGL((block_norm_backward<XT, YT, L, CH>), grid, dim3(std::max(L, 256)), 0, s, a, w_f32);
@@ -329,14 +361,14 @@ static void norm_go(const NormArgs &a, bool w_f32, hipStream_t s) {
     };
     std::integral_constant<int, 64> l64;
     std::integral_constant<int, 256> l256;
+    std::integral_constant<int, 512> l512;
     std::integral_constant<int, 1024> l1024;
     std::integral_constant<int, 1> c1;
     std::integral_constant<int, 2> c2;
     std::integral_constant<int, 8> c8;
     if (a.C <= 512) go(l64, c1);
-    else if (a.C <= 1024) go(l64, c2);
     else if (a.C <= 2048) go(l256, c1);
-    else if (a.C <= 4096) go(l256, c2);
+    else if (a.C <= 4096) go(l512, c1);
     else if (a.C <= 8192) go(l1024, c1);
     else if (a.C <= 16384) go(l1024, c2);
     else go(l1024, c8);
