@@ -1059,15 +1059,14 @@ def ft_router_backward(desc: dict, logits: torch.Tensor, topk_ids: Optional[torc
 
 # ------------------------------------------------------------ the routed experts in training, and norms
 
-@functools.lru_cache(maxsize=256)
-def _sort_struct(*values: int) -> ft_sort_desc_t:
-    return ft_sort_desc_t(*values)
+@functools.lru_cache(maxsize=256)   # a struct per set of values
+def _sort_struct(E, k, first, local, align, rows) -> ft_sort_desc_t:
+    return ft_sort_desc_t(int(E), int(k), int(first), int(E if local is None else local), int(align), int(rows))
 
 
 def _sort_desc(d: dict) -> ft_sort_desc_t:
     """``first`` and ``local`` may be left out (every expert is here)."""
-    E = int(d["n_experts"])
-    return _sort_struct(E, int(d["top_k"]), int(d.get("first", 0)), int(d.get("local", E)), int(d["align"]), int(d["rows"]))
+    return _sort_struct(d["n_experts"], d["top_k"], d.get("first", 0), d.get("local"), d["align"], d["rows"])
 
 
 def ft_expert_sort_rows(desc: dict, T: int) -> int:
@@ -1114,16 +1113,25 @@ def _need_tokens(d: ft_sort_desc_t, T: int, *features: int) -> None:
         raise FtError(FT_ERR_SHAPE, "sizes")
 
 
-def _sort_arg(dev: int, d: ft_sort_desc_t, T: int, sort, names):
-    """The tables ``names`` of a SortBuffers as an ft_sort_t, the others left out."""
+def _need_sort(sort) -> None:
     if not isinstance(sort, SortBuffers):
         raise ValueError(f"sort: expected a SortBuffers, got {type(sort).__name__}")
-    out = ft_sort_t()
-    for n in names:
-        size = {"row_pair": d.rows, "pair_row": T * d.top_k, "off": d.local + 1, "count": d.local, "dropped": 1}[n]
-        dev, at = _arg(dev, getattr(sort, n), n, _I32, size)
-        setattr(out, n, at)
-    return dev, ctypes.byref(out)
+
+
+def _groups_arg(dev: int, d: ft_sort_desc_t, sort):
+    """What a product reads of a SortBuffers, as an ft_sort_t."""
+    _need_sort(sort)
+    local = d.local
+    dev, off = _arg(dev, sort.off, "off", _I32, local + 1)
+    dev, count = _arg(dev, sort.count, "count", _I32, local)
+    return dev, ctypes.byref(ft_sort_t(None, None, off, count))
+
+
+def _pairs_arg(dev: int, d: ft_sort_desc_t, T: int, sort):
+    """What a call that goes by tokens reads of it."""
+    _need_sort(sort)
+    dev, at = _arg(dev, sort.pair_row, "pair_row", _I32, T * d.top_k)
+    return dev, ctypes.byref(ft_sort_t(None, at))
 
 
 def _optional(dev: int, t, name: str, dtypes: tuple, numel: int):
@@ -1139,10 +1147,17 @@ def ft_expert_sort(desc: dict, topk_ids: torch.Tensor, T: int, out: SortBuffers,
     if T > 0:
         dev, ip = _arg(dev, topk_ids, "topk_ids", _I32, T * d.top_k)
         dev, mp = _optional(dev, mask, "mask", _MASKS, T)
-    dev, sp = _sort_arg(dev, d, T, out, ("row_pair", "pair_row", "off", "count", "dropped") if T else
-                        ("row_pair", "off", "count", "dropped"))
+    _need_sort(out)
+    local, pairs = d.local, None
+    dev, rows = _arg(dev, out.row_pair, "row_pair", _I32, d.rows)
+    if T > 0:
+        dev, pairs = _arg(dev, out.pair_row, "pair_row", _I32, T * d.top_k)
+    dev, off = _arg(dev, out.off, "off", _I32, local + 1)
+    dev, count = _arg(dev, out.count, "count", _I32, local)
+    dev, dropped = _arg(dev, out.dropped, "dropped", _I32, 1)
     dev, wp = _arg(dev, ws, "ws", _BYTES, 0)
-    st = _on(dev, load().ft_expert_sort, ctypes.byref(d), ip, T, mp, sp, wp, ws.numel(), stream)
+    st = _on(dev, load().ft_expert_sort, ctypes.byref(d), ip, T, mp, ctypes.byref(ft_sort_t(rows, pairs, off, count, dropped)),
+             wp, ws.numel(), stream)
     _check(st, "ft_expert_sort")
 
 
@@ -1155,7 +1170,10 @@ def ft_expert_gather(desc: dict, sort: SortBuffers, x: torch.Tensor, T: int, C: 
     if T == 0:
         return
     dev, xp = _arg(-1, x, "x", _FLOAT_TYPES, T * C)
-    dev, sp = _sort_arg(dev, d, T, sort, ("row_pair", "off"))
+    _need_sort(sort)
+    dev, at = _arg(dev, sort.row_pair, "row_pair", _I32, d.rows)
+    dev, off = _arg(dev, sort.off, "off", _I32, d.local + 1)
+    sp = ctypes.byref(ft_sort_t(at, None, off))
     dev, wp = _optional(dev, weights, "weights", _F32, T * d.top_k)
     dev, pp = _optional(dev, rows, "rows", _FLOAT_TYPES, d.rows * C)
     dev, rp = _codes_arg(dev, row, "row", d.rows, C, True)
@@ -1173,7 +1191,7 @@ def ft_expert_combine(desc: dict, sort: SortBuffers, rows: torch.Tensor, T: int,
     if T == 0:
         return
     dev, rp = _arg(-1, rows, "rows", _FLOAT_TYPES, d.rows * C)
-    dev, sp = _sort_arg(dev, d, T, sort, ("pair_row",))
+    dev, sp = _pairs_arg(dev, d, T, sort)
     dev, yp = _arg(dev, y, "y", _FLOAT_TYPES, T * C)
     dev, wp = _optional(dev, weights, "weights", _F32, T * d.top_k)
     dev, bp = _optional(dev, base, "base", (y.dtype,), T * C)
@@ -1189,7 +1207,7 @@ def ft_expert_gate_grad(desc: dict, sort: SortBuffers, rows: torch.Tensor, dy: t
     if T == 0:
         return
     dev, rp = _arg(-1, rows, "rows", _FLOAT_TYPES, d.rows * C)
-    dev, sp = _sort_arg(dev, d, T, sort, ("pair_row",))
+    dev, sp = _pairs_arg(dev, d, T, sort)
     dev, yp = _arg(dev, dy, "dy", _FLOAT_TYPES, T * C)
     dev, wp = _arg(dev, d_weights, "d_weights", _F32, T * d.top_k)
     st = _on(dev, load().ft_expert_gate_grad, ctypes.byref(d), sp, rp, _FLOATS[rows.dtype], yp, _FLOATS[dy.dtype], T, C, wp,
@@ -1216,7 +1234,7 @@ def ft_expert_linear(desc: dict, linear: dict, weight: dict, x: ActCodes, sort: 
         raise FtError(FT_ERR_DTYPE, "ft_expert_linear")
     dev, w, s = _expert_weights(-1, weight, "weight", d.local, N, K)
     dev, xp = _codes_arg(dev, x, "x", d.rows, K)
-    dev, sp = _sort_arg(dev, d, T, sort, ("off", "count"))
+    dev, sp = _groups_arg(dev, d, sort)
     dev, yp = _arg(dev, y, "y", (_X_DTYPES[l.y_dtype],), d.rows * N)
     st = _on(dev, load().ft_expert_linear, ctypes.byref(d), ctypes.byref(l), w, s, xp, sp, T, yp, stream)
     _check(st, "ft_expert_linear")
@@ -1243,20 +1261,20 @@ def ft_expert_weight_grad(desc: dict, out_features: int, in_features: int, dy_co
     if T > 0:
         dev, yp = _codes_arg(dev, dy_col, "dy_col", N, d.rows)
         dev, xp = _codes_arg(dev, x_col, "x_col", K, d.rows)
-        dev, sp = _sort_arg(dev, d, T, sort, ("off", "count"))
+        dev, sp = _groups_arg(dev, d, sort)
     st = _on(dev, load().ft_expert_weight_grad, ctypes.byref(d), N, K, yp, xp, sp, T, out, _FLOATS[dw.dtype],
              1 if accumulate else 0, stream)
     _check(st, "ft_expert_weight_grad")
 
 
 @functools.lru_cache(maxsize=256)
-def _norm_struct(*values) -> ft_norm_desc_t:
-    return ft_norm_desc_t(*values)
+def _norm_struct(C, x, y, w, post, eps, scale) -> ft_norm_desc_t:
+    return ft_norm_desc_t(int(C), int(x), int(y), int(w), int(post), float(eps), float(scale))
 
 
 def _norm_desc(d: dict) -> ft_norm_desc_t:
-    return _norm_struct(int(d["channels"]), int(d["x_dtype"]), int(d["y_dtype"]), int(d["w_dtype"]), int(d.get("post_norm", 0)),
-                        float(d["eps"]), float(d.get("scale", 1.0)))
+    return _norm_struct(d["channels"], d["x_dtype"], d["y_dtype"], d["w_dtype"], d.get("post_norm", 0), d["eps"],
+                        d.get("scale", 1.0))
 
 
 def _norm_types(d: ft_norm_desc_t, T: int, where: str):
@@ -1269,12 +1287,12 @@ def _norm_types(d: ft_norm_desc_t, T: int, where: str):
 
 
 def _norm_params(dev: int, d: ft_norm_desc_t, T: int, params: dict, kind):
-    out = ft_norm_params_t()
-    for n in ("pre", "post", "gate"):
-        dev, at = _optional(dev, params.get(n), n, (kind,), d.channels)
-        setattr(out, n, at)
-    dev, out.token_gate = _optional(dev, params.get("token_gate"), "token_gate", _F32, T)
-    return dev, ctypes.byref(out)
+    C, kinds, at = d.channels, (kind,), [None] * 4
+    for i, n in enumerate(("pre", "post", "gate", "token_gate")):
+        t = params.get(n)
+        if t is not None:
+            dev, at[i] = _arg(dev, t, n, kinds if i < 3 else _F32, C if i < 3 else T)
+    return dev, ctypes.byref(ft_norm_params_t(*at))
 
 
 def ft_block_norm(desc: dict, params: dict, x: torch.Tensor, block: Optional[torch.Tensor], T: int,
@@ -1315,11 +1333,12 @@ def ft_block_norm_backward(desc: dict, params: dict, r: torch.Tensor, block: Opt
     """``grads``: float32 tensors for the gradients of ``params``, those left out or None are not formed."""
     d, T = _norm_desc(desc), int(T)
     xk, yk, wk = _norm_types(d, T, "ft_block_norm_backward")
-    size, g, dev = T * d.channels, ft_norm_grads_t(), -1
-    for n in ("pre", "post", "gate", "token_gate"):
-        dev, at = _optional(dev, (grads or {}).get(n), "d_" + n, _F32, T if n == "token_gate" else d.channels)
-        setattr(g, n, at)
-    if T == 0 and not (g.pre or g.post or g.gate):
+    size, g, dev = T * d.channels, [None] * 4, -1
+    for i, n in enumerate(("pre", "post", "gate", "token_gate")):
+        t = (grads or {}).get(n)
+        if t is not None:
+            dev, g[i] = _arg(dev, t, "d_" + n, _F32, d.channels if i < 3 else T)
+    if T == 0 and not any(g[:3]):
         return
     dev, pp = _norm_params(dev, d, T, params, wk)
     rp = bp = drp = dnp = dxp = dbp = None
@@ -1331,6 +1350,6 @@ def ft_block_norm_backward(desc: dict, params: dict, r: torch.Tensor, block: Opt
         dev, dxp = _optional(dev, dx, "dx", (xk,), size)
         dev, dbp = _optional(dev, d_block, "d_block", (yk,), size)
     dev, wp = _optional(dev, ws, "ws", _BYTES, 0)
-    st = _on(dev, load().ft_block_norm_backward, ctypes.byref(d), pp, rp, bp, drp, dnp, T, dxp, dbp, ctypes.byref(g), wp,
+    st = _on(dev, load().ft_block_norm_backward, ctypes.byref(d), pp, rp, bp, drp, dnp, T, dxp, dbp, ctypes.byref(ft_norm_grads_t(*g)), wp,
              0 if ws is None else ws.numel(), stream)
     _check(st, "ft_block_norm_backward")

@@ -46,17 +46,28 @@ __device__ __forceinline__ void zero_unless(bool in, float (&v)[N]) {
 #pragma unroll
         for (int q = 0; q < N; ++q) v[q] = 0.0f;
 }
+// A store of 8 or 16 bytes.  STREAM: of what no kernel reads again soon enough, past the caches, so that it neither
+// displaces what is read nor comes back to write it out.
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+template <bool STREAM, class V>
+__device__ __forceinline__ void put_words(void *p, V v) {
+    if constexpr (STREAM) __builtin_nontemporal_store(v, static_cast<V *>(p));
+    else *static_cast<V *>(p) = v;
+}
+
 // eight values out, rounded to nearest even where they are bf16 (one instruction for two; a NaN stays one)
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(a), static_cast<__bf16>(b)});
 }
+template <bool STREAM = false>
 __device__ __forceinline__ void store8(uint16_t *p, const float *v) {
-    *reinterpret_cast<uint4 *>(p) = uint4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
+    put_words<STREAM>(p, u32x4_t{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])});
 }
+template <bool STREAM = false>
 __device__ __forceinline__ void store8(float *p, const float *v) {
-    reinterpret_cast<float4 *>(p)[0] = float4{v[0], v[1], v[2], v[3]};
-    reinterpret_cast<float4 *>(p)[1] = float4{v[4], v[5], v[6], v[7]};
+    put_words<STREAM>(p, floatx4_t{v[0], v[1], v[2], v[3]});
+    put_words<STREAM>(p + 4, floatx4_t{v[4], v[5], v[6], v[7]});
 }
 template <class XT>
 __device__ __forceinline__ void load16(const XT *p, float (&v)[16]) {
@@ -69,7 +80,8 @@ __device__ __forceinline__ void load16(const XT *p, float (&v)[16]) {
 //
 // A column's scale depends on its largest magnitude only through the exponent and through whether the mantissa
 // is above 1.75: the upper 16 bits, rounded up, decide it exactly, so two columns share a word of LDS.
-template <int NP>
+// STREAM: the codes' stores do not stay in the caches.
+template <int NP, bool STREAM = false>
 __device__ __forceinline__ void put_tile(const float (&v)[NP][kActRows][8], ActTileShared<NP> &sh, const ActPlane (&to)[NP],
                                          int row0, int col_kb) {
     const int t = threadIdx.x, g = t / 16, sub = t % 16;
@@ -82,9 +94,9 @@ __device__ __forceinline__ void put_tile(const float (&v)[NP][kActRows][8], ActT
                 const int byte = act_scale_byte(block_mag16(v[n][r])), row = row0 + kActRows * g + r;
                 const float sc = act_scale_operand(byte);
                 if (row < f.R)
-                    *reinterpret_cast<uint2 *>(f.codes + static_cast<size_t>(row) * f.Kp + to[n].row_kb * 128 + 8 * sub) =
-                        uint2{act_codes4(v[n][r][0], v[n][r][1], v[n][r][2], v[n][r][3], sc),
-                              act_codes4(v[n][r][4], v[n][r][5], v[n][r][6], v[n][r][7], sc)};
+                    put_words<STREAM>(f.codes + static_cast<size_t>(row) * f.Kp + to[n].row_kb * 128 + 8 * sub,
+                                      u32x2_t{act_codes4(v[n][r][0], v[n][r][1], v[n][r][2], v[n][r][3], sc),
+                                              act_codes4(v[n][r][4], v[n][r][5], v[n][r][6], v[n][r][7], sc)});
                 if (sub == 0) sh.rowscale[n][kActRows * g + r] = static_cast<uint8_t>(byte);
             }
         }
@@ -139,8 +151,8 @@ __device__ __forceinline__ void put_tile(const float (&v)[NP][kActRows][8], ActT
             const int c = i / 8, p = i % 8;
             if (to[n].col_row0 + c < f.R) {
                 const uint32_t *s = reinterpret_cast<const uint32_t *>(sh.t[n] + c * kTPad + 16 * p);
-                *reinterpret_cast<uint4 *>(f.codes + static_cast<size_t>(to[n].col_row0 + c) * f.Kp + col_kb * 128 + 16 * p) =
-                    uint4{s[0], s[1], s[2], s[3]};
+                put_words<STREAM>(f.codes + static_cast<size_t>(to[n].col_row0 + c) * f.Kp + col_kb * 128 + 16 * p,
+                                  u32x4_t{s[0], s[1], s[2], s[3]});
             }
         }
         if (t >= 64 && t < 72)

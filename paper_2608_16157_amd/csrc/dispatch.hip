@@ -87,7 +87,7 @@ __global__ __launch_bounds__(kActThreads) void gather_tiles(RowsArgs a, const XT
         zero_unless(t[r] >= 0 && c < a.C, v[0][r]);   // C is a multiple of 16
     }
     const ActPlane to[1] = {{row, cb, col, cb * 128}};
-    put_tile<1>(v, sh, to, rb * 128, rb);
+    put_tile<1, true>(v, sh, to, rb * 128, rb);
 }
 
 template <class XT>
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(256) void combine_rows(RowsArgs a, const RT *rows, 
             for (int q = 0; q < 8; ++q) sum[q] = fmaf(f, v[j][q], sum[q]);
         }
     }
-    store8(y + static_cast<size_t>(t) * a.C + c, sum);
+    store8<true>(y + static_cast<size_t>(t) * a.C + c, sum);
 }
 
 hipError_t launch_combine(const RowsArgs &a, const void *rows, bool rows_f32, const void *base, void *y, bool y_f32, hipStream_t s) {

@@ -7,6 +7,7 @@
 #include "product_tile.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace ftmoe {
 
@@ -86,7 +87,7 @@ __global__ __launch_bounds__(64 * GA * GB, 2) void expert_tiled(ProductArgs p, G
         zero_tile<OUT>(p.out, p.M, ta * BA, min((ta + 1) * BA, p.M), t.row, t.end);
         return;
     }
-    lds_tile<WA, WB, GA, GB, 0, WIDE, OUT, true>(of_expert(p, g, t), ta * BA, t.row, 0, p.Kp / 128, t.end);
+    lds_tile<WA, WB, GA, GB, 0, WIDE, OUT, true, (BB >= 128)>(of_expert(p, g, t), ta * BA, t.row, 0, p.Kp / 128, t.end);
 }
 
 template <int RA, int TB, int W, bool WIDE, int OUT>
@@ -108,9 +109,12 @@ __global__ __launch_bounds__(64 * W) void expert_direct(ProductArgs p, GroupArgs
 template <int WA, int WB, int GA, int GB, bool WIDE, int OUT>
 __global__ __launch_bounds__(64 * GA * GB, 2) void expert_grad(ProductArgs p, GroupArgs g, int na, int nb) {
     constexpr int BA = 16 * WA * GA, BB = 16 * WB * GB;
-    const int L = xcd_remap(blockIdx.x, g.n * na * nb), e = L / (na * nb);
-    int ta, tb;
-    tile_at(L - e * (na * nb), na, nb, ta, tb);
+    // Patches of kBand B tiles by all A tiles go over the XCDs in turn: groups of unlike sizes then keep all of them busy.
+    constexpr int kBand = 4;
+    const int bands = (nb + kBand - 1) / kBand, i = blockIdx.x / 8, turn = i / (kBand * na), at = i - turn * (kBand * na);
+    const int patch = turn * 8 + blockIdx.x % 8, e = patch / bands, band = patch - e * bands, bw = min(kBand, nb - band * kBand);
+    if (e >= g.n || at >= bw * na) return;
+    const int ta = at / bw, tb = band * kBand + at % bw;
     int o = 0, blocks = 0;   // without tables there are no rows
     if (g.off) {
         o = group_start(g, e);
@@ -121,7 +125,7 @@ __global__ __launch_bounds__(64 * GA * GB, 2) void expert_grad(ProductArgs p, Gr
         if constexpr (OUT != 2) zero_tile<OUT>(p.out, p.M, ta * BA, min((ta + 1) * BA, p.M), tb * BB, min((tb + 1) * BB, p.R));
         return;
     }
-    lds_tile<WA, WB, GA, GB, 1, WIDE, OUT, false>(p, ta * BA, tb * BB, o / 128, o / 128 + blocks, 0);
+    lds_tile<WA, WB, GA, GB, 1, WIDE, OUT, false, true>(p, ta * BA, tb * BB, o / 128, o / 128 + blocks, 0);
 }
 
 // Most tiles of bb rows that the groups can make: each is a multiple of align rows, and their sum is within the rows.
@@ -145,11 +149,19 @@ static void direct(const ProductArgs &p, const GroupArgs &g, long pairs, hipStre
     hipLaunchKernelGGL((expert_direct<RA, TB, W, WIDE, OUT>), dim3(na, nb), dim3(64 * W), 0, s, p, g);
 }
 
+// Which kernel, by the rows that a group holds on average (in order: direct 32 x 16, 128 x 64, 128 x 128, 256 x 256; us).
+// 128 experts of 1536 x 2048, bf16, mean 1: 43.8 46.5 47.9 70.6; 4: 69.4 75.7 79.9 110; 8: 84.9 82.3 85.8 113; 32: 169 89.7
+// 93.6 140; 64: 333 126 108 144; 64 of them, 192: - 112 86.8 94.4; 384: - 165 128 127; 512: - 208 160 145.  32 of
+// 7168 x 2048, 256: - 256 197 205; 512: - 423 319 300.  float32, mean 1: 45.1 52.1 63.2; 4: 73.5 84.7 103; 16: 112 97.8 117;
+// 64: 336 151 142.  A product of few features fills the card with 128 x 128 only: 8 of 576 x 4096, mean 1024: 36.4 against
+// 51.5.  Direct tiles of 16 x 16, 16 x 32, 32 x 32 and 64 x 16, of 4 and 8 waves, and 64 x 64 through LDS were never more
+// than 2 % better than the best of these.
 template <bool WIDE, int OUT>
 static hipError_t product(const ProductArgs &p, const GroupArgs &g, long pairs, float mean, hipStream_t s) {
-    if (mean <= 16) direct<1, 1, 8, WIDE, OUT>(p, g, pairs, s);
+    const float largest = static_cast<float>((p.M + 255) / 256) * g.n * std::ceil(mean / 256);   // tiles of 256 x 256
+    if (mean <= 6) direct<2, 1, 4, WIDE, OUT>(p, g, pairs, s);
     else if (mean <= 48) tiled<4, 2, 2, 2, WIDE, OUT>(p, g, pairs, s);
-    else if (WIDE || mean <= 128) tiled<4, 4, 2, 2, WIDE, OUT>(p, g, pairs, s);
+    else if (WIDE || mean <= 384 || largest < 192) tiled<4, 4, 2, 2, WIDE, OUT>(p, g, pairs, s);
     else if constexpr (!WIDE) tiled<8, 4, 2, 4, WIDE, OUT>(p, g, pairs, s);
     return hipGetLastError();
 }
@@ -161,7 +173,8 @@ hipError_t launch_expert_product(const ProductArgs &p, const GroupArgs &g, long 
 template <int WA, int WB, int GA, int GB, bool WIDE, int OUT>
 static void grad(const ProductArgs &p, const GroupArgs &g, hipStream_t s) {
     const int na = (p.M + 16 * WA * GA - 1) / (16 * WA * GA), nb = (p.R + 16 * WB * GB - 1) / (16 * WB * GB);
-    hipLaunchKernelGGL((expert_grad<WA, WB, GA, GB, WIDE, OUT>), dim3(g.n * na * nb), dim3(64 * GA * GB), 0, s, p, g, na, nb);
+    const int patches = g.n * ((nb + 3) / 4);
+    hipLaunchKernelGGL((expert_grad<WA, WB, GA, GB, WIDE, OUT>), dim3((patches + 7) / 8 * 8 * 4 * na), dim3(64 * GA * GB), 0, s, p, g, na, nb);
 }
 
 hipError_t launch_expert_weight_grad(const ProductArgs &p, const GroupArgs &g, int out, hipStream_t s) {

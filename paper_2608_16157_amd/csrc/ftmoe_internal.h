@@ -88,10 +88,11 @@ struct SortArgs {
     int pairs, k, first, n, align, rows;
     int32_t *row_pair, *pair_row, *off, *count, *dropped;
     int chunk, blocks;      // pairs a workgroup places, workgroups
-    int32_t *table;         // [n][blocks] pairs of an expert in a workgroup's chunk, then in those before it
+    int32_t *table;         // [blocks][n] pairs of an expert in a workgroup's chunk, then in those before it
     int32_t *totals;        // [n]
 };
-constexpr int kSortPairs = 4096;     // pairs that a workgroup holds at once
+constexpr int kSortPairs = 2048;     // pairs that a workgroup holds at once
+constexpr int kSortOwnSums = 64;     // workgroups up to which each sums up the counts before its own
 constexpr int kSortMaxBlocks = 1024;
 
 // Rows in the order of the groups, and back (dispatch.hip).

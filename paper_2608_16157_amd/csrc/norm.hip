@@ -269,7 +269,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES == 1024 ? 4 : 3) v
                 sb[i][q] = fmaf(n[i][q], r[i][q] * rr, sb[i][q]);
                 sa[i][q] = fmaf(hb * d[i][q], b[i][q], sa[i][q]);
             }
-            if (in[i] && a.r) store8(static_cast<XT *>(a.r) + at + c[i], d[i]);
+            if (in[i] && a.r) store8<true>(static_cast<XT *>(a.r) + at + c[i], d[i]);
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
                 d[i][q] *= kHold ? up[kHold ? i : 0][q] : wu[q];   // scale gate post d
@@ -285,7 +285,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES == 1024 ? 4 : 3) v
         for (int i = 0; i < CH; ++i) {
 #pragma unroll
             for (int q = 0; q < 8; ++q) d[i][q] = hb * fmaf(-off, b[i][q], d[i][q]);
-            if (in[i]) store8(static_cast<YT *>(a.nout) + at + c[i], d[i]);
+            if (in[i]) store8<true>(static_cast<YT *>(a.nout) + at + c[i], d[i]);
         }
     }
     if (!a.parts) return;

@@ -260,7 +260,8 @@ __device__ __forceinline__ void again(const ProductArgs &p, int a0, int b0, int 
 // data 2 and its way through L2 (81 % hits, two patches of tiles compared) nothing.  32 x 32 instructions,
 // behind which the scale hides whole, draw more power: 206 us at the same busy share and a lower clock.
 // Tile at rows a0 of A and b0 of B, blocks [k0, k1), k1 > k0.  GROUPED: the rows from p.R up to `end` are stored as zeros.
-template <int WA, int WB, int GA, int GB, int ASC, bool WIDE, int OUT, bool GROUPED>
+// STREAM: the results' stores do not stay in the caches.
+template <int WA, int WB, int GA, int GB, int ASC, bool WIDE, int OUT, bool GROUPED, bool STREAM>
 __device__ __forceinline__ void lds_tile(ProductArgs p, int a0, int b0, int k0, int k1, int end) {
     constexpr bool kWide = WIDE;
     constexpr int NW = GA * GB, BA = 16 * WA * GA, BB = 16 * WB * GB, HS = WA / 2;   // HS steps per half
@@ -530,6 +531,7 @@ __device__ __forceinline__ void lds_tile(ProductArgs p, int a0, int b0, int k0, 
             if (bi < (GROUPED ? end : p.R) && ai < p.M) {
                 u32x4_t *o = reinterpret_cast<u32x4_t *>(static_cast<uint8_t *>(split_out(p)) + (static_cast<size_t>(bi) * p.M + ai) * kSize);
                 if constexpr (OUT == 2) *reinterpret_cast<floatx4_t *>(o) += __builtin_bit_cast(floatx4_t, v);
+                else if constexpr (STREAM) __builtin_nontemporal_store(v, o);
                 else *o = v;
             }
         }
@@ -551,7 +553,7 @@ __global__ __launch_bounds__(64 * GA * GB, 2) void product_tiled(ProductArgs p, 
     int ta, tb, k0, k1;
     tile_at(xcd_remap(blockIdx.x, na * nb), na, nb, ta, tb);
     split_range(p, p.Kp / 128, k0, k1);
-    lds_tile<WA, WB, GA, GB, ASC, WIDE, OUT, false>(p, ta * 16 * WA * GA, tb * 16 * WB * GB, k0, k1, 0);
+    lds_tile<WA, WB, GA, GB, ASC, WIDE, OUT, false, false>(p, ta * 16 * WA * GA, tb * 16 * WB * GB, k0, k1, 0);
 }
 
 }  // namespace ftmoe

@@ -5,9 +5,9 @@
 // the waves of a workgroup from their counts in LDS, across workgroups from a table of counts.  No atomic decides a
 // place, so equal calls give equal tables.
 //
-// Up to kSortPairs pairs: one launch of one workgroup.  More: counts per workgroup, their prefix sums per expert, and
-// the placing, in which every workgroup forms the groups' starts for itself from the totals.
-// Bound: launches and round trips.
+// Up to kSortPairs pairs: one launch of one workgroup.  More: counts per workgroup, and the placing, in which every
+// workgroup sums up the counts before its own and forms the groups' starts for itself; past kSortOwnSums workgroups a
+// launch between the two turns the counts into sums.  Bound: launches and round trips.
 #include "ftmoe_device.h"
 #include "ftmoe_internal.h"
 
@@ -22,27 +22,42 @@ __device__ __forceinline__ int sort_key(const SortArgs &a, int p) {
     return in ? static_cast<int>(e) : a.n;
 }
 
+// rows without a pair are what the placing leaves of this
+__device__ __forceinline__ void sort_clear(const SortArgs &a) {
+    for (int r = blockIdx.x * kSortThreads + threadIdx.x; r < a.rows; r += gridDim.x * kSortThreads) a.row_pair[r] = -1;
+}
+
 __global__ __launch_bounds__(kSortThreads) void sort_count(SortArgs a) {
     extern __shared__ int hist[];   // [n + 1]
-    for (int e = threadIdx.x; e <= a.n; e += kSortThreads) hist[e] = 0;
-    __syncthreads();
     const int p0 = blockIdx.x * a.chunk, p1 = min(p0 + a.chunk, a.pairs);
-    for (int p = p0 + threadIdx.x; p < p1; p += kSortThreads) atomicAdd(&hist[sort_key(a, p)], 1);
+    for (int e = threadIdx.x; e <= a.n; e += kSortThreads) hist[e] = 0;
+    sort_clear(a);
     __syncthreads();
-    for (int e = threadIdx.x; e < a.n; e += kSortThreads) a.table[static_cast<size_t>(e) * a.blocks + blockIdx.x] = hist[e];
+    for (int sub = p0; sub < p1; sub += kSortPairs) {
+        int key[kSortSteps];
+#pragma unroll
+        for (int i = 0; i < kSortSteps; ++i) {
+            const int p = sub + i * kSortThreads + threadIdx.x;
+            key[i] = p < p1 ? sort_key(a, p) : a.n;
+        }
+#pragma unroll
+        for (int i = 0; i < kSortSteps; ++i) atomicAdd(&hist[key[i]], 1);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.n; e += kSortThreads) a.table[static_cast<size_t>(blockIdx.x) * a.n + e] = hist[e];
 }
 
 // one wave per expert: its counts become the counts before each workgroup
 __global__ __launch_bounds__(64) void sort_prefix(SortArgs a) {
-    int32_t *row = a.table + static_cast<size_t>(blockIdx.x) * a.blocks;
+    int32_t *col = a.table + blockIdx.x;
     const int per = (a.blocks + 63) / 64, b0 = min(static_cast<int>(threadIdx.x) * per, a.blocks), b1 = min(b0 + per, a.blocks);
     uint32_t sum = 0;
-    for (int b = b0; b < b1; ++b) sum += row[b];
+    for (int b = b0; b < b1; ++b) sum += col[static_cast<size_t>(b) * a.n];
     const uint32_t upto = wave_incl_scan_u32(sum);
     uint32_t before = upto - sum;
     for (int b = b0; b < b1; ++b) {
-        const uint32_t v = row[b];
-        row[b] = static_cast<int32_t>(before);
+        const uint32_t v = col[static_cast<size_t>(b) * a.n];
+        col[static_cast<size_t>(b) * a.n] = static_cast<int32_t>(before);
         before += v;
     }
     if (threadIdx.x == 63) a.totals[blockIdx.x] = static_cast<int32_t>(upto);
@@ -54,8 +69,10 @@ __global__ __launch_bounds__(kSortThreads) void sort_place(SortArgs a, int nbits
     int *off = hist + kSortWaves * a.n;       // [n + 1] groups' starts
     int *end = off + a.n + 1;                 // [n] one past the last row with a pair
     int *run = end + a.n;                     // [n] totals, then the next row to fill
+    int *lead = run + a.n;                    // [n] pairs in the workgroups before this one
     const int t = threadIdx.x, wave = t / 64, lane = lane_id();
     const bool whole = a.blocks == 1;
+    if (whole) sort_clear(a);
     const int p0 = blockIdx.x * a.chunk, p1 = min(p0 + a.chunk, a.pairs);
     bool first = true;
     for (int sub = p0; first || sub < p1; sub += kSortPairs) {
@@ -84,12 +101,23 @@ __global__ __launch_bounds__(kSortThreads) void sort_place(SortArgs a, int nbits
         __syncthreads();
         if (first) {
             for (int e = t; e < a.n; e += kSortThreads) {
-                int sum = 0;
-                if (whole)
+                int sum = 0, mine = 0;
+                if (whole) {
+#pragma unroll
                     for (int w = 0; w < kSortWaves; ++w) sum += hist[w * a.n + e];
-                else
+                } else if (a.blocks > kSortOwnSums) {
                     sum = a.totals[e];
+                    mine = a.table[static_cast<size_t>(blockIdx.x) * a.n + e];
+                } else {
+#pragma unroll 8
+                    for (int b = 0; b < a.blocks; ++b) {
+                        const int v = a.table[static_cast<size_t>(b) * a.n + e];
+                        sum += v;
+                        mine += b < static_cast<int>(blockIdx.x) ? v : 0;
+                    }
+                }
                 run[e] = sum;
+                lead[e] = mine;
             }
             __syncthreads();
             if (wave == 0) {
@@ -115,15 +143,11 @@ __global__ __launch_bounds__(kSortThreads) void sort_place(SortArgs a, int nbits
             }
             __syncthreads();
             for (int e = t; e < a.n; e += kSortThreads) {
-                run[e] = off[e] + (whole ? 0 : a.table[static_cast<size_t>(e) * a.blocks + blockIdx.x]);
+                run[e] = off[e] + lead[e];
                 if (blockIdx.x == 0) a.count[e] = end[e] - off[e];
             }
             if (blockIdx.x == 0)
                 for (int e = t; e <= a.n; e += kSortThreads) a.off[e] = off[e];
-            // rows without a pair
-            for (int e = blockIdx.x * kSortWaves + wave; e < a.n; e += gridDim.x * kSortWaves)
-                for (int r = end[e] + lane; r < off[e + 1]; r += 64) a.row_pair[r] = -1;
-            for (int r = off[a.n] + blockIdx.x * kSortThreads + t; r < a.rows; r += gridDim.x * kSortThreads) a.row_pair[r] = -1;
             first = false;
         }
         __syncthreads();
@@ -156,11 +180,11 @@ __global__ __launch_bounds__(kSortThreads) void sort_place(SortArgs a, int nbits
 hipError_t launch_sort(const SortArgs &a, hipStream_t s) {
     if (a.blocks > 1) {
         hipLaunchKernelGGL(sort_count, dim3(a.blocks), dim3(kSortThreads), (a.n + 1) * 4, s, a);
-        hipLaunchKernelGGL(sort_prefix, dim3(a.n), dim3(64), 0, s, a);
+        if (a.blocks > kSortOwnSums) hipLaunchKernelGGL(sort_prefix, dim3(a.n), dim3(64), 0, s, a);
     }
     int nbits = 1;
     while ((1 << nbits) < a.n) ++nbits;   // of the keys that have an expert here
-    const unsigned lds = ((kSortWaves + 3) * a.n + 1) * 4;
+    const unsigned lds = ((kSortWaves + 4) * a.n + 1) * 4;
     hipLaunchKernelGGL(sort_place, dim3(a.blocks), dim3(kSortThreads), lds, s, a, nbits);
     return hipGetLastError();
 }

@@ -184,7 +184,7 @@ def test_binding_refuses_before_the_call():
         with pytest.raises(ValueError, match="device"):
             call()
     with pytest.raises(ValueError, match="SortBuffers"):
-        ftm._sort_arg(-1, ftm._sort_desc(d), 4, None, ("off",))
+        ftm._groups_arg(-1, ftm._sort_desc(d), None)
     for call in (lambda: ftm.ft_expert_gather(d, s, x, 4, 100, row=c), lambda: ftm.ft_expert_combine(d, s, x, -1, 128, x),
                  lambda: ftm.ft_expert_linear_transpose(0, 128, 128, wt, wt), lambda: ftm.ft_block_norm({**nd, "x_dtype": 4}, {}, x, None, 4),
                  lambda: ftm.ft_expert_linear(d, {**lin, "x_dtype": 1}, wt, c, s, 4, x),
