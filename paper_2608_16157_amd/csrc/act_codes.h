@@ -130,4 +130,10 @@ __device__ __forceinline__ uint32_t f32_to_bf16_any(float f) {
     return f != f ? 0x7FC0u : (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
 }
 
+// two of them in one instruction, a in the low half; a NaN keeps its sign and payload, made quiet
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(a), static_cast<__bf16>(b)});
+}
+
 }  // namespace ftmoe

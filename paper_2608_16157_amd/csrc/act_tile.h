@@ -28,14 +28,24 @@ struct ActPlane {
     int col_row0;
 };
 
+// A store of 8 or 16 bytes.  STREAM: of what no kernel reads again soon enough, past the caches, so that it neither
+// displaces what is read nor comes back to write it out.
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+template <bool STREAM, class V>
+__device__ __forceinline__ void put_words(void *p, V v) {
+    if constexpr (STREAM) __builtin_nontemporal_store(v, static_cast<V *>(p));
+    else *static_cast<V *>(p) = v;
+}
+
 // One block of a row by 8 lanes, 16 values a lane; rows past T (zeros, up to f.Rp) leave only their scale byte.
+template <bool STREAM = false>
 __device__ __forceinline__ void put_row(const float (&v)[16], const ActForm &f, long row, int T, int kb, int sub) {
     const int byte = act_scale_byte(block_mag8(v));
     const float sc = act_scale_operand(byte);
     if (row < T)
-        *reinterpret_cast<uint4 *>(f.codes + static_cast<size_t>(row) * f.Kp + kb * 128 + 16 * sub) =
-            uint4{act_codes4(v[0], v[1], v[2], v[3], sc), act_codes4(v[4], v[5], v[6], v[7], sc),
-                  act_codes4(v[8], v[9], v[10], v[11], sc), act_codes4(v[12], v[13], v[14], v[15], sc)};
+        put_words<STREAM>(f.codes + static_cast<size_t>(row) * f.Kp + kb * 128 + 16 * sub,
+                          u32x4_t{act_codes4(v[0], v[1], v[2], v[3], sc), act_codes4(v[4], v[5], v[6], v[7], sc),
+                                  act_codes4(v[8], v[9], v[10], v[11], sc), act_codes4(v[12], v[13], v[14], v[15], sc)});
     if (sub == 0) f.scales[static_cast<size_t>(kb) * f.Rp + row] = static_cast<uint8_t>(byte);
 }
 // Values outside the matrix are read from inside it (p is clamped by the caller) and dropped here: a load
@@ -46,20 +56,7 @@ __device__ __forceinline__ void zero_unless(bool in, float (&v)[N]) {
 #pragma unroll
         for (int q = 0; q < N; ++q) v[q] = 0.0f;
 }
-// A store of 8 or 16 bytes.  STREAM: of what no kernel reads again soon enough, past the caches, so that it neither
-// displaces what is read nor comes back to write it out.
-typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
-template <bool STREAM, class V>
-__device__ __forceinline__ void put_words(void *p, V v) {
-    if constexpr (STREAM) __builtin_nontemporal_store(v, static_cast<V *>(p));
-    else *static_cast<V *>(p) = v;
-}
-
-// eight values out, rounded to nearest even where they are bf16 (one instruction for two; a NaN stays one)
-__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(a), static_cast<__bf16>(b)});
-}
+// eight values out, rounded to nearest even where they are bf16
 template <bool STREAM = false>
 __device__ __forceinline__ void store8(uint16_t *p, const float *v) {
     put_words<STREAM>(p, u32x4_t{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])});

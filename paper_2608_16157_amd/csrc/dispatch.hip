@@ -19,33 +19,48 @@ __device__ __forceinline__ int row_token(const RowsArgs &a, long row, float &w) 
 // one past the last group's rows
 __device__ __forceinline__ int rows_end(const RowsArgs &a) { return min(a.off[a.n], a.rows); }
 
-// Plain rows: one wave per row.
+// Block of 128 columns and block of `rows` rows of a workgroup, the columns outermost: what runs together on an XCD then
+// reads the same columns, of all tokens (2 MB of 8192 in bf16), and each is read from memory once however many rows want
+// it.  False past the groups' rows.
+__device__ __forceinline__ bool gather_place(const RowsArgs &a, int rows, int &cb, int &rb, int &end) {
+    end = rows_end(a);
+    const int nkb = (a.C + 127) / 128, nrb = (end + rows - 1) / rows;
+    if (end <= 0 || static_cast<long>(blockIdx.x) >= static_cast<long>(nkb) * nrb) return false;
+    const int L = xcd_remap(blockIdx.x, nkb * nrb);
+    cb = L / nrb;
+    rb = L - cb * nrb;
+    return true;
+}
+
+// Plain rows: 16 lanes per (row, block of 128), four rows on the way at once.
 template <class XT, class OT>
 __global__ __launch_bounds__(256) void gather_plain(RowsArgs a, const XT *x, OT *out) {
-    const long row = static_cast<long>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    if (row >= rows_end(a)) return;
-    float w;
-    const int t = row_token(a, row, w);
-    const XT *from = x + static_cast<size_t>(max(t, 0)) * a.C;
-    OT *to = out + static_cast<size_t>(row) * a.C;
-#pragma unroll 4
-    for (int c = 8 * lane_id(); c < a.C; c += 512) {
-        float v[8];
-        load8(from + c, v);
-        zero_unless(t >= 0, v);
+    int cb, rb, end;
+    if (!gather_place(a, 64, cb, rb, end)) return;
+    const int c = cb * 128 + 8 * (threadIdx.x % 16), row0 = rb * 64 + threadIdx.x / 16;
+    float v[4][8], w[4];
+    int t[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) t[r] = row_token(a, min(row0 + 16 * r, end - 1), w[r]);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) load8(x + static_cast<size_t>(max(t[r], 0)) * a.C + min(c, a.C - 8), v[r]);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
         if (a.w)
 #pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] *= w;
-        store8(to + c, v);
+            for (int q = 0; q < 8; ++q) v[r][q] *= w[r];
+        zero_unless(t[r] >= 0, v[r]);
+        if (row0 + 16 * r < end && c < a.C) store8<true>(out + static_cast<size_t>(row0 + 16 * r) * a.C + c, v[r]);
     }
 }
 
 // The row form alone: 8 lanes per (row, block of 128), two rows on the way at once.
 template <class XT>
 __global__ __launch_bounds__(256) void gather_rows(RowsArgs a, const XT *x, ActForm f) {
-    const int sub = threadIdx.x % 8, kb = blockIdx.x, c = kb * 128 + 16 * sub, end = rows_end(a);
-    const long row0 = static_cast<long>(blockIdx.y) * 64 + threadIdx.x / 8;
-    if (blockIdx.y * 64L >= end) return;
+    int kb, rb, end;
+    if (!gather_place(a, 64, kb, rb, end)) return;
+    const int sub = threadIdx.x % 8, c = kb * 128 + 16 * sub;
+    const long row0 = rb * 64L + threadIdx.x / 8;
     float v[2][16], w[2];
     int t[2];
 #pragma unroll
@@ -59,7 +74,7 @@ __global__ __launch_bounds__(256) void gather_rows(RowsArgs a, const XT *x, ActF
 #pragma unroll
             for (int q = 0; q < 16; ++q) v[r][q] *= w[r];
         zero_unless(t[r] >= 0 && c < a.C, v[r]);   // C is a multiple of 16
-        if (row0 + 32 * r < end) put_row(v[r], f, row0 + 32 * r, end, kb, sub);
+        if (row0 + 32 * r < end) put_row<true>(v[r], f, row0 + 32 * r, end, kb, sub);
     }
 }
 
@@ -68,9 +83,8 @@ template <class XT>
 __global__ __launch_bounds__(kActThreads) void gather_tiles(RowsArgs a, const XT *x, ActForm row, ActForm col) {
     __shared__ __attribute__((aligned(16))) ActTileShared<1> sh;
     const int g = threadIdx.x / 16, sub = threadIdx.x % 16;
-    const int nkb = (a.C + 127) / 128, nrb = rows_end(a) / 128;
-    if (static_cast<int>(blockIdx.x) >= nkb * nrb) return;
-    const int L = xcd_remap(blockIdx.x, nkb * nrb), cb = L / nrb, rb = L - cb * nrb;
+    int cb, rb, end;
+    if (!gather_place(a, 128, cb, rb, end)) return;
     const int row0 = rb * 128 + kActRows * g, c = cb * 128 + 8 * sub;
     float v[1][kActRows][8], w[kActRows];
     int t[kActRows];
@@ -94,7 +108,7 @@ template <class XT>
 static void gather(const RowsArgs &a, const XT *x, void *plain, bool plain_f32, const ActForm &row, const ActForm &col,
                    hipStream_t s) {
     if (plain) {
-        const dim3 grid((a.rows + 3) / 4);
+        const dim3 grid((a.C + 127) / 128 * ((a.rows + 63) / 64));
         if (plain_f32)
             hipLaunchKernelGGL((gather_plain<XT, float>), grid, dim3(256), 0, s, a, x, static_cast<float *>(plain));
         else
@@ -104,7 +118,7 @@ static void gather(const RowsArgs &a, const XT *x, void *plain, bool plain_f32, 
     if (col.codes)
         hipLaunchKernelGGL(gather_tiles<XT>, dim3(nkb * (a.rows / 128)), dim3(kActThreads), 0, s, a, x, row, col);
     else if (row.codes)
-        hipLaunchKernelGGL(gather_rows<XT>, dim3(nkb, (a.rows + 63) / 64), dim3(256), 0, s, a, x, row);
+        hipLaunchKernelGGL(gather_rows<XT>, dim3(nkb * ((a.rows + 63) / 64)), dim3(256), 0, s, a, x, row);
 }
 
 hipError_t launch_gather(const RowsArgs &a, const void *x, bool x_f32, void *plain, bool plain_f32, const ActForm &row,

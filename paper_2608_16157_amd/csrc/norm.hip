@@ -61,92 +61,12 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*buf)[N][16], int
     }
 }
 
-__device__ __forceinline__ float over_rms(float sum, const NormArgs &a) { return 1.0f / sqrtf(sum / a.C + a.eps); }
-
-template <class XT, class YT, int LANES, int CH>
-__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void block_norm(NormArgs a, bool w_f32) {
-    constexpr int kRows = LANES < 256 ? 256 / LANES : 1;   // rows of a workgroup at once
-    constexpr bool kHold = CH <= 2;                        // weights stay in registers
-    __shared__ float buf[2][1][16];
-    int turn = 0;
-    const int lane = threadIdx.x % LANES;
-    int c[CH];
-    bool in[CH];
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-        c[i] = (i * LANES + lane) * 8;
-        in[i] = c[i] < a.C;
-    }
-    float pre[kHold ? CH : 1][8], up[kHold ? CH : 1][8];   // up: scale gate post
-    auto weights = [&](int i, float *wp, float *wu) {
-        float g[8];
-        const int at = min(c[i], a.C - 8);
-        channels8(a.pre, w_f32, at, wp);
-        channels8(a.post_norm ? a.post : nullptr, w_f32, at, wu);
-        channels8(a.gate, w_f32, at, g);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) wu[q] *= a.scale * g[q];
-    };
-    if constexpr (kHold)
-#pragma unroll
-        for (int i = 0; i < CH; ++i) weights(i, pre[i], up[i]);
-    for (long row = static_cast<long>(blockIdx.x) * kRows + threadIdx.x / LANES; row < a.T; row += static_cast<long>(gridDim.x) * kRows) {
-        const size_t at = static_cast<size_t>(row) * a.C;
-        float x[CH][8], b[CH][8];
-#pragma unroll
-        for (int i = 0; i < CH; ++i) load8(static_cast<const XT *>(a.x) + at + min(c[i], a.C - 8), x[i]);
-        if (a.b) {
-#pragma unroll
-            for (int i = 0; i < CH; ++i) load8(static_cast<const YT *>(a.b) + at + min(c[i], a.C - 8), b[i]);
-            float h = a.tgate ? a.tgate[row] : 1.0f;
-            if (a.post_norm) {
-                float s[1] = {0.0f};
-#pragma unroll
-                for (int i = 0; i < CH; ++i)
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) s[0] = fmaf(in[i] ? b[i][q] : 0.0f, b[i][q], s[0]);
-                row_sums<LANES, 1>(s, buf, turn);
-                h *= over_rms(s[0], a);
-            }
-#pragma unroll
-            for (int i = 0; i < CH; ++i) {
-                float wp[8], wu[8];
-                if constexpr (!kHold) weights(i, wp, wu);
-#pragma unroll
-                for (int q = 0; q < 8; ++q) x[i][q] = fmaf(kHold ? up[kHold ? i : 0][q] : wu[q], b[i][q] * h, x[i][q]);
-                if (in[i] && a.r) store8(static_cast<XT *>(a.r) + at + c[i], x[i]);
-            }
-        }
-        if (!a.nout && !a.row.codes) continue;
-        float s[1] = {0.0f};
-#pragma unroll
-        for (int i = 0; i < CH; ++i)
-#pragma unroll
-            for (int q = 0; q < 8; ++q) s[0] = fmaf(in[i] ? x[i][q] : 0.0f, x[i][q], s[0]);
-        row_sums<LANES, 1>(s, buf, turn);
-        const float rr = over_rms(s[0], a);
-#pragma unroll
-        for (int i = 0; i < CH; ++i) {
-            float wp[8], wu[8], n[8];
-            if constexpr (!kHold) weights(i, wp, wu);
-#pragma unroll
-            for (int q = 0; q < 8; ++q) n[q] = in[i] ? x[i][q] * rr * (kHold ? pre[kHold ? i : 0][q] : wp[q]) : 0.0f;
-            if (in[i] && a.nout) store8(static_cast<YT *>(a.nout) + at + c[i], n);
-            if (a.row.codes && c[i] < a.row.Kp) {   // Kp is a multiple of 128: whole lane rows of 16
-                const int byte = act_scale_byte(block_mag16(n));
-                const float sc = act_scale_operand(byte);
-                *reinterpret_cast<uint2 *>(a.row.codes + static_cast<size_t>(row) * a.row.Kp + c[i]) =
-                    uint2{act_codes4(n[0], n[1], n[2], n[3], sc), act_codes4(n[4], n[5], n[6], n[7], sc)};
-                if (lane % 16 == 0) a.row.scales[static_cast<size_t>(c[i] / 128) * a.row.Rp + row] = static_cast<uint8_t>(byte);
-            }
-        }
-    }
-    // scales of the rows that fill the form up
-    if (a.row.codes && blockIdx.x == 0) {
-        const int more = a.row.Rp - a.T;
-        for (int i = threadIdx.x; i < more * (a.row.Kp / 128); i += blockDim.x)
-            a.row.scales[static_cast<size_t>(i / more) * a.row.Rp + a.T + i % more] = 127;
-    }
+// 1 / rms.  All channels of a token share its error, so the two roundings of 1 / sqrt(m) are taken back by a Newton step
+// whose residual 1 - m y^2 is exact to float32's square.
+__device__ __forceinline__ float over_rms(float sum, const NormArgs &a) {
+    const float m = sum / a.C + a.eps, y = 1.0f / sqrtf(m), t = m * y;
+    const float left = fmaf(-t, y, 1.0f) - fmaf(m, y, -t) * y;
+    return isfinite(left) ? fmaf(0.5f * y, left, y) : y;   // rows of zeros without eps, and what is not finite: as it is
 }
 
 // 8 channels as they lie in memory, and their values
@@ -175,12 +95,114 @@ __device__ __forceinline__ void values8(const Raw8<T> &r, float *v) {
         v[q] = __uint_as_float(sizeof(T) == 4 ? w[q] : q % 2 ? w[q / 2] & 0xFFFF0000u : w[q / 2] << 16);
 }
 
+template <class XT, class YT, int LANES, int CH>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES == 1024 ? 4 : 5) void block_norm(NormArgs a, bool w_f32) {
+    constexpr int kRows = LANES < 256 ? 256 / LANES : 1;   // rows of a workgroup at once
+    constexpr bool kHold = CH == 1;                        // weights stay in registers
+    __shared__ float buf[2][1][16];
+    int turn = 0;
+    const int lane = threadIdx.x % LANES;
+    int c[CH];
+    bool in[CH];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        c[i] = (i * LANES + lane) * 8;
+        in[i] = c[i] < a.C;
+    }
+    float pre[kHold ? CH : 1][8], up[kHold ? CH : 1][8];   // up: scale gate post
+    auto weights = [&](int i, float *wp, float *wu) {
+        float g[8];
+        const int at = min(c[i], a.C - 8);
+        channels8(a.pre, w_f32, at, wp);
+        channels8(a.post_norm ? a.post : nullptr, w_f32, at, wu);
+        channels8(a.gate, w_f32, at, g);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) wu[q] *= a.scale * g[q];
+    };
+    if constexpr (kHold)
+#pragma unroll
+        for (int i = 0; i < CH; ++i) weights(i, pre[i], up[i]);
+    const long first = static_cast<long>(blockIdx.x) * kRows + threadIdx.x / LANES, stride = static_cast<long>(gridDim.x) * kRows;
+    Raw8<XT> x8[CH];
+    Raw8<YT> b8[CH] = {};
+    float h8 = 1.0f;
+    auto request = [&](long row) {   // of rows past the last one: the last one, unused
+        row = min(row, a.T - 1L);
+        const size_t at = static_cast<size_t>(row) * a.C;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) fetch8<XT>(a.x, at + min(c[i], a.C - 8), x8[i]);
+        if (a.b)
+#pragma unroll
+            for (int i = 0; i < CH; ++i) fetch8<YT>(a.b, at + min(c[i], a.C - 8), b8[i]);
+        if (a.tgate) h8 = a.tgate[row];
+    };
+    request(first);
+    for (long row = first; row < a.T; row += stride) {
+        const size_t at = static_cast<size_t>(row) * a.C;
+        float x[CH][8], b[CH][8], h = h8;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            values8(x8[i], x[i]);
+            values8(b8[i], b[i]);
+        }
+        request(row + stride);
+        if (a.b) {
+            if (a.post_norm) {
+                float s[1] = {0.0f};
+#pragma unroll
+                for (int i = 0; i < CH; ++i)
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) s[0] = fmaf(in[i] ? b[i][q] : 0.0f, b[i][q], s[0]);
+                row_sums<LANES, 1>(s, buf, turn);
+                h *= over_rms(s[0], a);
+            }
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                float wp[8], wu[8];
+                if constexpr (!kHold) weights(i, wp, wu);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) x[i][q] = fmaf(kHold ? up[kHold ? i : 0][q] : wu[q], b[i][q] * h, x[i][q]);
+                if (in[i] && a.r) store8<true>(static_cast<XT *>(a.r) + at + c[i], x[i]);
+            }
+        }
+        if (!a.nout && !a.row.codes) continue;
+        float s[1] = {0.0f};
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) s[0] = fmaf(in[i] ? x[i][q] : 0.0f, x[i][q], s[0]);
+        row_sums<LANES, 1>(s, buf, turn);
+        const float rr = over_rms(s[0], a);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            float wp[8], wu[8], n[8];
+            if constexpr (!kHold) weights(i, wp, wu);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) n[q] = in[i] ? x[i][q] * rr * (kHold ? pre[kHold ? i : 0][q] : wp[q]) : 0.0f;
+            if (in[i] && a.nout) store8<true>(static_cast<YT *>(a.nout) + at + c[i], n);
+            if (a.row.codes && c[i] < a.row.Kp) {   // Kp is a multiple of 128: whole lane rows of 16
+                const int byte = act_scale_byte(block_mag16(n));
+                const float sc = act_scale_operand(byte);
+                *reinterpret_cast<uint2 *>(a.row.codes + static_cast<size_t>(row) * a.row.Kp + c[i]) =
+                    uint2{act_codes4(n[0], n[1], n[2], n[3], sc), act_codes4(n[4], n[5], n[6], n[7], sc)};
+                if (lane % 16 == 0) a.row.scales[static_cast<size_t>(c[i] / 128) * a.row.Rp + row] = static_cast<uint8_t>(byte);
+            }
+        }
+    }
+    // scales of the rows that fill the form up
+    if (a.row.codes && blockIdx.x == 0) {
+        const int more = a.row.Rp - a.T;
+        for (int i = threadIdx.x; i < more * (a.row.Kp / 128); i += blockDim.x)
+            a.row.scales[static_cast<size_t>(i / more) * a.row.Rp + a.T + i % more] = 127;
+    }
+}
+
 // A row's channels of a thread; the next row's are requested before the sums of this one are waited for: a workgroup
 // of 1024 threads fills a CU.  Up to 8192 channels nothing spills.
 template <class XT, class YT, int LANES, int CH>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES == 1024 ? 4 : 3) void block_norm_backward(NormArgs a, bool w_f32) {
     constexpr int kRows = LANES < 256 ? 256 / LANES : 1;
-    constexpr bool kHold = CH <= 2;
+    constexpr bool kHold = CH == 1;    // weights stay in registers, and the next row is on its way
     __shared__ float buf3[2][3][16], buf1[2][1][16];
     int turn3 = 0, turn1 = 0;
     const int lane = threadIdx.x % LANES;
@@ -229,8 +251,9 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES == 1024 ? 4 : 3) v
             for (int i = 0; i < CH; ++i) fetch8<XT>(a.dr, at + min(c[i], a.C - 8), d8[i]);
         if (a.tgate) h8 = a.tgate[row];
     };
-    request(part);
+    if (kHold) request(part);
     for (long row = part; row < a.T; row += stride) {
+        if (!kHold) request(row);
         const size_t at = static_cast<size_t>(row) * a.C;
         float r[CH][8], n[CH][8], b[CH][8], d[CH][8], s[3] = {0.0f, 0.0f, 0.0f};
         const float h = h8;
@@ -241,7 +264,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES == 1024 ? 4 : 3) v
             values8(b8[i], b[i]);
             values8(d8[i], d[i]);
         }
-        request(row + stride);
+        if (kHold) request(row + stride);
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             float wp[8], wu[8];
@@ -347,7 +370,7 @@ static NormShape norm_shape(int C) {
 // Workgroups: as many as run at once, so that each holds its weights for several rows and leaves one part.
 static int norm_blocks(int T, int C, bool back) {
     const NormShape n = norm_shape(C);
-    return std::min((T + n.rows - 1) / n.rows, back ? 256 * 1024 / std::max(n.lanes, 256) : 512 * 1024 / std::max(n.lanes, 256));
+    return std::min((T + n.rows - 1) / n.rows, (back || n.lanes == 1024 ? 256 : 384) * 1024 / std::max(n.lanes, 256));
 }
 int norm_parts(int T, int C) { return norm_blocks(T, C, true) * norm_shape(C).rows; }
 

@@ -516,7 +516,9 @@ __device__ __forceinline__ void lds_tile(ProductArgs p, int a0, int b0, int k0, 
 #pragma unroll
         for (int i = 0; i < WA; ++i) {
             uint8_t *at = mine + r * kPitch + (16 * i + 4 * g) * kSize;
-            if constexpr (OUT == 0)
+            if constexpr (OUT == 0 && (GROUPED || STREAM))
+                *reinterpret_cast<uint2 *>(at) = uint2{bf16_pair(acc[i][j][0], acc[i][j][1]), bf16_pair(acc[i][j][2], acc[i][j][3])};
+            else if constexpr (OUT == 0)
                 *reinterpret_cast<uint2 *>(at) = uint2{f32_to_bf16_any(acc[i][j][0]) | f32_to_bf16_any(acc[i][j][1]) << 16,
                                                        f32_to_bf16_any(acc[i][j][2]) | f32_to_bf16_any(acc[i][j][3]) << 16};
             else *reinterpret_cast<floatx4_t *>(at) = acc[i][j];
