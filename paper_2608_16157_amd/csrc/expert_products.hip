@@ -149,20 +149,32 @@ static void direct(const ProductArgs &p, const GroupArgs &g, long pairs, hipStre
     hipLaunchKernelGGL((expert_direct<RA, TB, W, WIDE, OUT>), dim3(na, nb), dim3(64 * W), 0, s, p, g);
 }
 
-// Which kernel, by the rows that a group holds on average (in order: direct 32 x 16, 128 x 64, 128 x 128, 256 x 256; us).
-// 128 experts of 1536 x 2048, bf16, mean 1: 43.8 46.5 47.9 70.6; 4: 69.4 75.7 79.9 110; 8: 84.9 82.3 85.8 113; 32: 169 89.7
-// 93.6 140; 64: 333 126 108 144; 64 of them, 192: - 112 86.8 94.4; 384: - 165 128 127; 512: - 208 160 145.  32 of
-// 7168 x 2048, 256: - 256 197 205; 512: - 423 319 300.  float32, mean 1: 45.1 52.1 63.2; 4: 73.5 84.7 103; 16: 112 97.8 117;
-// 64: 336 151 142.  A product of few features fills the card with 128 x 128 only: 8 of 576 x 4096, mean 1024: 36.4 against
-// 51.5.  Direct tiles of 16 x 16, 16 x 32, 32 x 32 and 64 x 16, of 4 and 8 waves, and 64 x 64 through LDS were never more
-// than 2 % better than the best of these.
+// Which kernel, by the rows that a group holds on average.  In order: direct 32 x 16; through LDS 128 x 64, 128 x 128,
+// 256 x 128, 256 x 256 (us):
+//   128 experts of 1536 x 2048, bf16    mean 1: 43.8 46.5 47.9 - 70.6;  4: 69.4 75.7 79.9 - 110;  8: 84.9 82.3 85.8 - 113;
+//                                       32: 169 89.7 93.6 - 140;  64: 333 126 109 104 132;  128: - 153 125 121 138
+//   64 of 1536 x 2048, bf16             256: - 119 93.1 91.1 98.6;  384: - - 135 121 124;  512: - 200 155 152 137
+//   32 of 2048 x 7168, bf16             192: - - 171 154 191;  256: - 241 192 176 196;  512: - 382 296 283 267
+//   128 of 1536 x 2048, float32         mean 1: 45.1 52.1 63.2;  4: 73.5 84.7 103;  16: 112 97.8 117;  64: 336 151 142 151
+// Where the tiles of 128 x 128 fill the card no more than twice, or are odd in number along the features, the larger ones lose:
+// 8 of 576 x 4096, mean 1024: 34.1 50.9 49.6; 16 of 400 x 1040, mean 64: 10.8 13.5 18.8.  Direct tiles of 16 x 16, 16 x 32,
+// 32 x 32 and 64 x 16, of 4 and 8 waves, and 64 x 64 and 128 x 256 through LDS were never more than 2 % better.
 template <bool WIDE, int OUT>
 static hipError_t product(const ProductArgs &p, const GroupArgs &g, long pairs, float mean, hipStream_t s) {
-    const float largest = static_cast<float>((p.M + 255) / 256) * g.n * std::ceil(mean / 256);   // tiles of 256 x 256
-    if (mean <= 6) direct<2, 1, 4, WIDE, OUT>(p, g, pairs, s);
-    else if (mean <= 48) tiled<4, 2, 2, 2, WIDE, OUT>(p, g, pairs, s);
-    else if (WIDE || mean <= 384 || largest < 192) tiled<4, 4, 2, 2, WIDE, OUT>(p, g, pairs, s);
-    else if constexpr (!WIDE) tiled<8, 4, 2, 4, WIDE, OUT>(p, g, pairs, s);
+    const int a128 = (p.M + 127) / 128;
+    const float small = static_cast<float>(a128) * g.n * std::ceil(mean / 128);                                   // tiles of 128 x 128
+    const float largest = static_cast<float>((p.M + 255) / 256) * g.n * std::ceil(mean / 256);   // of 256 x 256
+    if (mean <= 6) {
+        direct<2, 1, 4, WIDE, OUT>(p, g, pairs, s);
+    } else if (mean <= 48) {
+        tiled<4, 2, 2, 2, WIDE, OUT>(p, g, pairs, s);
+    } else if constexpr (WIDE) {
+        tiled<4, 4, 2, 2, WIDE, OUT>(p, g, pairs, s);
+    } else {
+        if (mean > 384 && largest >= 192) tiled<8, 4, 2, 4, WIDE, OUT>(p, g, pairs, s);
+        else if (a128 % 2 == 0 && small >= 512) tiled<4, 4, 4, 2, WIDE, OUT>(p, g, pairs, s);
+        else tiled<4, 4, 2, 2, WIDE, OUT>(p, g, pairs, s);
+    }
     return hipGetLastError();
 }
 
@@ -177,8 +189,12 @@ static void grad(const ProductArgs &p, const GroupArgs &g, hipStream_t s) {
     hipLaunchKernelGGL((expert_grad<WA, WB, GA, GB, WIDE, OUT>), dim3((patches + 7) / 8 * 8 * 4 * na), dim3(64 * GA * GB), 0, s, p, g, na, nb);
 }
 
-hipError_t launch_expert_weight_grad(const ProductArgs &p, const GroupArgs &g, int out, hipStream_t s) {
-    if (out == 0) grad<8, 4, 2, 4, false, 0>(p, g, s);
+// Short reductions want small tiles, whose loads and stores overlap between the two of a CU (128 x 128 against 256 x 256,
+// bf16, mean 4, 94, 256, 512 and 1024 rows: 220 190 588 415 224 and 256 240 556 386 217 us; 256 x 128 lies between them
+// or above).  float32 results, whose operands are widened in registers: 128 x 128 was best of 128 x 64, 256 x 64 and 256 x 128.
+hipError_t launch_expert_weight_grad(const ProductArgs &p, const GroupArgs &g, float mean, int out, hipStream_t s) {
+    if (out == 0 && mean <= 192) grad<4, 4, 2, 2, false, 0>(p, g, s);
+    else if (out == 0) grad<8, 4, 2, 4, false, 0>(p, g, s);
     else if (out == 1) grad<4, 4, 2, 2, true, 1>(p, g, s);
     else grad<4, 4, 2, 2, true, 2>(p, g, s);
     return hipGetLastError();

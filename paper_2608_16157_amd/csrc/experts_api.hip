@@ -257,7 +257,8 @@ ft_status_t ft_expert_weight_grad(const ft_sort_desc_t *desc, int32_t out_featur
     p.asr = pad128(in_features);
     p.bsr = pad128(out_features);
     const int out = dw_dtype == FT_DT_BF16 ? 0 : accumulate ? 2 : 1;
-    return done(launch_expert_weight_grad(p, g, out, static_cast<hipStream_t>(stream)));
+    const float mean = static_cast<float>(T) * desc->top_k / desc->n_experts;
+    return done(launch_expert_weight_grad(p, g, mean, out, static_cast<hipStream_t>(stream)));
 }
 
 ft_status_t ft_block_norm(const ft_norm_desc_t *desc, const ft_norm_params_t *params, const void *x, const void *block,

@@ -465,7 +465,7 @@ hipError_t launch_combine(const RowsArgs &a, const void *rows, bool rows_f32, co
 hipError_t launch_gate_grad(const RowsArgs &a, const void *rows, bool rows_f32, const void *dy, bool dy_f32, float *d_w, hipStream_t s);
 // pairs: the most that the groups can hold, mean: expected in one of them; out as for launch_product
 hipError_t launch_expert_product(const ProductArgs &p, const GroupArgs &g, long pairs, float mean, int out, hipStream_t s);
-hipError_t launch_expert_weight_grad(const ProductArgs &p, const GroupArgs &g, int out, hipStream_t s);
+hipError_t launch_expert_weight_grad(const ProductArgs &p, const GroupArgs &g, float mean, int out, hipStream_t s);
 // parts of the column sums that a backward pass leaves (NormArgs.n_parts)
 int norm_parts(int T, int C);
 hipError_t launch_block_norm(const NormArgs &a, bool x_f32, bool y_f32, bool w_f32, hipStream_t s);

@@ -226,11 +226,20 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES == 1024 ? 4 : 3) v
     if constexpr (kHold)
 #pragma unroll
         for (int i = 0; i < CH; ++i) weights(i, pre[i], up[i]);
-    float sa[CH][8], sb[CH][8];   // A and B over this workgroup's rows
+    // A and B over this workgroup's rows, each channel its thread's own: in registers, or, where those are short, in LDS
+    constexpr bool kInLds = CH == 2;
+    __shared__ __attribute__((aligned(16))) float column[kInLds ? 2 * LANES * CH * 8 : 4];
+    float sa[kInLds ? 1 : CH][8], sb[kInLds ? 1 : CH][8];
+    auto columns = [&](int i, int which) { return reinterpret_cast<floatx4_t *>(column + (which * CH + i) * LANES * 8 + lane * 8); };
+    if constexpr (kInLds) {
 #pragma unroll
-    for (int i = 0; i < CH; ++i)
+        for (int i = 0; i < 2 * CH; ++i) columns(i, 0)[0] = columns(i, 0)[1] = floatx4_t{};
+    } else {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) sa[i][q] = sb[i][q] = 0.0f;
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) sa[i][q] = sb[i][q] = 0.0f;
+    }
     const long part = static_cast<long>(blockIdx.x) * kRows + threadIdx.x / LANES, stride = static_cast<long>(gridDim.x) * kRows;
     Raw8<XT> r8[CH], d8[CH] = {};
     Raw8<YT> b8[CH] = {}, n8[CH] = {};
@@ -289,9 +298,23 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES == 1024 ? 4 : 3) v
             for (int q = 0; q < 8; ++q) {
                 const float g = n[i][q] * (kHold ? pre[kHold ? i : 0][q] : wp[q]);
                 if (a.dn) d[i][q] = fmaf(rr, fmaf(-mean, r[i][q], g), d[i][q]);
-                sb[i][q] = fmaf(n[i][q], r[i][q] * rr, sb[i][q]);
-                sa[i][q] = fmaf(hb * d[i][q], b[i][q], sa[i][q]);
+                if constexpr (!kInLds) {
+                    sb[i][q] = fmaf(n[i][q], r[i][q] * rr, sb[i][q]);
+                    sa[i][q] = fmaf(hb * d[i][q], b[i][q], sa[i][q]);
+                }
             }
+            if constexpr (kInLds)
+#pragma unroll
+                for (int v = 0; v < 2; ++v) {
+                    floatx4_t ca = columns(i, 0)[v], cb = columns(i, 1)[v];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        ca[q] = fmaf(hb * d[i][4 * v + q], b[i][4 * v + q], ca[q]);
+                        cb[q] = fmaf(n[i][4 * v + q], r[i][4 * v + q] * rr, cb[q]);
+                    }
+                    columns(i, 0)[v] = ca;
+                    columns(i, 1)[v] = cb;
+                }
             if (in[i] && a.r) store8<true>(static_cast<XT *>(a.r) + at + c[i], d[i]);
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
@@ -316,8 +339,16 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES == 1024 ? 4 : 3) v
 #pragma unroll
     for (int i = 0; i < CH; ++i)
         if (in[i]) {
-            store8(mine + c[i], sa[i]);
-            store8(mine + a.C + c[i], sb[i]);
+            if constexpr (kInLds)
+#pragma unroll
+                for (int v = 0; v < 2; ++v) {
+                    *reinterpret_cast<floatx4_t *>(mine + c[i] + 4 * v) = columns(i, 0)[v];
+                    *reinterpret_cast<floatx4_t *>(mine + a.C + c[i] + 4 * v) = columns(i, 1)[v];
+                }
+            else {
+                store8(mine + c[i], sa[i]);
+                store8(mine + a.C + c[i], sb[i]);
+            }
         }
 }
 
