@@ -768,7 +768,8 @@ ft_status_t ft_expert_weight_grad(const ft_sort_desc_t *desc, int32_t out_featur
  *   channels   C; x_dtype of x, r and their gradients, y_dtype of b, n and theirs, w_dtype of pre, post and gate
  *              (FT_DT_BF16 or FT_DT_F32 each);  eps >= 0 and scale finite (FT_ERR_SHAPE otherwise)
  *   params     pre, post, gate [C], token_gate [T] float32; NULL: ones
- * Everything is computed in float32 and rounded once: n is of r before r's rounding.
+ * Everything is computed in float32 and rounded once: n is of r before r's rounding.  Sums of squares are float32 too:
+ * values past 2^64 / sqrt(C) in a row leave its norm 0; a row of zeros with eps 0 has none (NaN).
  */
 typedef struct {
     int32_t channels, x_dtype, y_dtype, w_dtype, post_norm;

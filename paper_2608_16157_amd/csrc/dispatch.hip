@@ -6,6 +6,9 @@
 #include "act_tile.h"
 #include "gemm_tile.h"
 
+#include <algorithm>
+#include <type_traits>
+
 namespace ftmoe {
 
 // The token of a row and the factor of its values: (-1, 0) where the row has no pair.
@@ -134,7 +137,8 @@ constexpr int kPairsOnWay = 8;
 
 template <class RT, class YT>
 __global__ __launch_bounds__(256) void combine_rows(RowsArgs a, const RT *rows, const YT *base, YT *y, int cblocks) {
-    const int t = blockIdx.x / cblocks, c = (blockIdx.x - t * cblocks) * 2048 + 8 * threadIdx.x;
+    const int block = blockIdx.y * gridDim.x + blockIdx.x, t = block / cblocks, c = (block - t * cblocks) * 2048 + 8 * threadIdx.x;
+    if (t >= a.T) return;
     if (c >= a.C) return;
     float sum[8];
     if (base) load8(base + static_cast<size_t>(t) * a.C + c, sum);
@@ -164,8 +168,11 @@ __global__ __launch_bounds__(256) void combine_rows(RowsArgs a, const RT *rows, 
 }
 
 hipError_t launch_combine(const RowsArgs &a, const void *rows, bool rows_f32, const void *base, void *y, bool y_f32, hipStream_t s) {
-    const int cblocks = (a.C + 2047) / 2048;
-    const dim3 grid(static_cast<unsigned>(a.T) * cblocks);
+    // a token's blocks follow each other (all tokens' first blocks first: 216 us in place of 205 for 8192 x 7168); past
+    // 2^23 of them into the second dimension, which holds a launch's threads below 2^32
+    const int cblocks = (a.C + 2047) / 2048, blocks = a.T * cblocks;   // at most 2^25
+    constexpr int kMost = 1 << 23;
+    const dim3 grid(std::min(blocks, kMost), (blocks + kMost - 1) / kMost);
     auto go = [&](auto *r, auto *o) {
         using RT = std::remove_pointer_t<decltype(r)>;
         using YT = std::remove_pointer_t<decltype(o)>;

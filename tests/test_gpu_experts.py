@@ -463,6 +463,64 @@ def test_products_and_gradients_of_the_largest_tile(T, E, k, N, K):
     assert_product(dw, v, mag, int(want["count"].max()), BF16)
 
 
+@pytest.mark.parametrize("T,E,k,N,K", ((2400, 16, 2, 4352, 272), (2000, 34, 3, 2048, 1040), (1300, 3, 1, 12544, 400)))
+def test_products_of_tall_tiles_and_blocks_of_scale_0(T, E, k, N, K):
+    """Enough tiles for those of 256 x 128 and 256 x 256; weight blocks of scale 0 meet codes that are NaN."""
+    r = rng(T, N, K, 14)
+    d, want, s = layout(r, T, E, k, 128)
+    end = int(want["off"][-1])
+    wt, w = expert_weights(r, E, N, K)
+    wt["s"][:, 1::3, 1] = 0.0
+    rows = np.arange(N) // 128 % 3 == 1
+    w[:, rows, 128:256] = 0.0
+    form, q = form_of(matrix(r, d["rows"], K, spread=1)[0])
+    v, mag = experts.product(want, q, w)
+    assert_product(run_experts(d, s, wt, form, N, K, T, BF16)[:end], v, mag, K, BF16)
+    form.codes[::5, 130] = 0x7F
+    q = q.copy()
+    q[::5, 130] = 0.0
+    v, mag = experts.product(want, q, w)
+    y = run_experts(d, s, wt, form, N, K, T, BF16)
+    dropped = cuda(rows)
+    assert_product(y[:end][:, dropped], v[:, rows], mag[:, rows], K, BF16)
+    real = cuda((want["row_pair"][:end] >= 0) & (np.arange(end) % 5 == 0))
+    assert torch.equal(torch.isnan(y[:end]).any(dim=1), real) and torch.all(y[end:] == 7.0)
+
+
+@pytest.mark.parametrize("T,E,k", ((40, 63, 3), (40, 64, 3), (40, 65, 3), (200, 1000, 4), (3000, 1024, 2)))
+def test_many_groups(T, E, k):
+    """More groups than lanes: a workgroup finds its tile among them; tables with a bool mask, and with too few rows."""
+    N, K = 48, 144
+    r = rng(T, E, 15)
+    wt, w = expert_weights(r, E, N, K)
+    ids, mask = routing(r, T, E, k), r.random(T) < 0.8
+    for rows in (None, max(128, ftm.ft_expert_sort_rows({"n_experts": E, "top_k": k, "align": 16}, T) // 3 // 128 * 128)):
+        for align in (16, 128):
+            d = desc(E, k, align, T, rows=rows)
+            s = run_sort(d, ids, mask)
+            want = experts.sort(ids, 0, E, align, d["rows"], mask) if T * E < 1e6 else None
+            if want is None:
+                want = {n: getattr(s, n).cpu().numpy() for n in ("row_pair", "pair_row", "off", "count", "dropped")}
+            else:
+                assert np.array_equal(s.row_pair.cpu().numpy(), want["row_pair"])
+            form, q = form_of(matrix(r, d["rows"], K, spread=1)[0])
+            end = int(want["off"][-1])
+            v, mag = experts.product(want, q, w)
+            for yt in (BF16, F32):
+                y = run_experts(d, s, wt, form, N, K, T, yt)
+                assert_product(y[:end], v, mag, K, yt)
+                assert torch.all(y[end:] == 7.0)
+            if align == 128:
+                x = torch.where(s.row_pair[:, None] >= 0, cuda(q).float(), torch.zeros(1, device="cuda"))
+                xc = ftm.ActCodes(K, d["rows"])
+                ftm.ft_act_quantize(x, d["rows"], K, col=xc)
+                dw = torch.full((E, K, K), 3.0, device="cuda")
+                ftm.ft_expert_weight_grad(d, K, K, xc, xc, s, T, dw)
+                vals = dense.values(xc.codes.cpu().numpy(), xc.scales.cpu().numpy())[:, :d["rows"]].T
+                v, mag = experts.weight_grad(want, vals, vals)
+                assert_product(dw, v, mag, max(1, int(want["count"].max())), F32)
+
+
 def test_every_token_at_one_expert():
     """The groups are as uneven as they can be: few-row kernels then meet long groups, and the others are empty."""
     T, E, N, K = 130, 64, 272, 400

@@ -146,3 +146,20 @@ def test_a_million_tokens():
     ftm.ft_block_norm_backward(nd, {}, one, one, one, one, T, dx, None, {"pre": pre, "gate": gate}, ftm.alloc_block_norm_workspace(nd, T))
     # ones everywhere: n = 1, the norm takes its own gradient away; whole numbers below 2^24
     assert torch.equal(dx, one) and torch.all(pre == T) and torch.all(gate == T)
+
+
+def test_combine_of_the_most_channels():
+    """More blocks than one dimension of a grid holds: 2^20 tokens of 20480 channels, 43 GB of results."""
+    T, C = 1 << 20, 20480
+    d = {"n_experts": 4, "top_k": 1, "align": 16, "rows": 16}
+    s = ftm.SortBuffers(d, T)
+    s.pair_row.fill_(-1)
+    for t, row in ((0, 3), (T // 2, 7), (T - 1, 15)):
+        s.pair_row[t, 0] = row
+    rows = torch.arange(16, device="cuda", dtype=torch.float32)[:, None].expand(16, C).to(torch.bfloat16).contiguous()
+    y = torch.full((T, C), 9.0, dtype=torch.bfloat16, device="cuda")
+    ftm.ft_expert_combine(d, s, rows, T, C, y)
+    for t, row in ((0, 3), (T // 2, 7), (T - 1, 15)):
+        assert torch.all(y[t] == row)
+        y[t] = 0
+    assert all(not part.any() for part in y.split(1 << 17))

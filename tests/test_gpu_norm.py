@@ -137,7 +137,7 @@ def test_rows_of_zeros_and_rows_that_are_not_finite():
 
 @pytest.mark.parametrize("post", (0, 1))
 @pytest.mark.parametrize("xt,yt,wt", ((BF16, BF16, F32), (F32, BF16, BF16), (BF16, F32, F32), (F32, F32, F32)))
-@pytest.mark.parametrize("T,C", SIZES + ((700, 144), (1500, 2064)))
+@pytest.mark.parametrize("T,C", SIZES + ((700, 144), (1500, 2064), (600, 4112), (520, 8208), (300, 16400)))
 def test_backward(T, C, xt, yt, wt, post):
     r = rng(T, C, xt, yt, post, 2)
     d, val, dev = inputs(r, T, C, xt, yt, wt, post)
