@@ -2,7 +2,9 @@
 // gradient of the gates (ft_expert_gate_grad).  row_pair and pair_row come from sort.hip; what lies outside their
 // ranges counts as no pair and no row.
 //
-// All of these move memory once and compute little: the bound is HBM.
+// All of these move memory and compute little: the bound is HBM, and for the gather the L2, from which a row is read as often
+// as the token has experts.  8192 tokens of 7168 channels, 8 experts each (62000 to 65536 rows, 78000 to 82000 with padding): both forms
+// 277 us, the row form 205, plain rows 285; back to the tokens 204 us, 5.1 TB/s; the gates 190.
 #include "act_tile.h"
 #include "gemm_tile.h"
 
@@ -24,7 +26,8 @@ __device__ __forceinline__ int rows_end(const RowsArgs &a) { return min(a.off[a.
 
 // Block of 128 columns and block of `rows` rows of a workgroup, the columns outermost: what runs together on an XCD then
 // reads the same columns, of all tokens (2 MB of 8192 in bf16), and each is read from memory once however many rows want
-// it.  False past the groups' rows.
+// it (both forms of 8192 x 7168, 8 experts a token, with the sort: 347 us; two, four and eight blocks of columns side by side 363, 370, 361;
+// rows outermost 440).  False past the groups' rows.
 __device__ __forceinline__ bool gather_place(const RowsArgs &a, int rows, int &cb, int &rb, int &end) {
     end = rows_end(a);
     const int nkb = (a.C + 127) / 128, nrb = (end + rows - 1) / rows;

@@ -14,14 +14,13 @@
 // is read once.  Row sums: lanes of a wave, then the waves in order through LDS.  Column sums: a thread's own over the rows
 // of its workgroup, then over the workgroups in order, in float64.
 //
-// The bound is HBM.
+// The bound is HBM: forward with a norm on both sides 8192 x 7168 bf16 112 us, 4.7 TB/s; backward 150 us and 5 for the join, 4.6 TB/s.
 #include "act_tile.h"
 
 #include <algorithm>
 #include <type_traits>
 
 namespace ftmoe {
-
 
 // 8 channels of a weight or gate; ones where there is none
 __device__ __forceinline__ void channels8(const void *w, bool f32, int c, float *v) {
@@ -197,8 +196,10 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES == 1024 ? 4 : 5) v
     }
 }
 
-// A row's channels of a thread; the next row's are requested before the sums of this one are waited for: a workgroup
-// of 1024 threads fills a CU.  Up to 8192 channels nothing spills.
+// A row's channels of a thread; up to 8192 channels the next row's are requested before the sums of this one are waited for: a
+// workgroup of 1024 threads fills a CU, and without its next row on the way nothing is (8192 x 7168: 324 us; 16 channels a
+// thread and half the threads spill).  Up to 16384 channels the weights are read again for every row and the column sums
+// lie in LDS (3500 x 16384: 517 us with all of it in registers, 388 without the weights, 246 so); beyond, registers spill.
 template <class XT, class YT, int LANES, int CH>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES == 1024 ? 4 : 3) void block_norm_backward(NormArgs a, bool w_f32) {
     constexpr int kRows = LANES < 256 ? 256 / LANES : 1;

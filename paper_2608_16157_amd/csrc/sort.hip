@@ -7,7 +7,9 @@
 //
 // Up to kSortPairs pairs: one launch of one workgroup.  More: counts per workgroup, and the placing, in which every
 // workgroup sums up the counts before its own and forms the groups' starts for itself; past kSortOwnSums workgroups a
-// launch between the two turns the counts into sums.  Bound: launches and round trips.
+// launch between the two turns the counts into sums.  Bound: launches and round trips: 32 pairs 4.5 us, 2048 7.4, 65536 11.7,
+// 786432 17.0.  One wave per expert that clears the rows behind its pairs, in place of clearing all of them ahead of the
+// counts: 7.2 us for 32 pairs of 256 experts.
 #include "ftmoe_device.h"
 #include "ftmoe_internal.h"
 
