@@ -17,7 +17,7 @@ __device__ __forceinline__ int group_start(const GroupArgs &g, int e) {
 }
 
 struct GroupTile {
-    int e, row, real, end, total;   // expert, first row, one past its last row with a pair and past its last row; tiles in all
+    int e, row, real, end;   // expert, first row, one past its last row with a pair and past its last row
 };
 
 // Tile t of BB rows, in the order of the experts.  Every wave finds it for itself: 64 lanes hold up to 16 experts each.
@@ -106,15 +106,52 @@ __global__ __launch_bounds__(64 * W) void expert_direct(ProductArgs p, GroupArgs
     direct_tile<RA, TB, W, 0, 0, WIDE, OUT, true>(of_expert(p, g, t), ta * BA, t.row, 0, p.Kp / 128, t.end);
 }
 
-template <int WA, int WB, int GA, int GB, bool WIDE, int OUT>
+// Groups of few rows lie a few hundred bytes wide in each row of the column forms.  Read as their tiles come, memory serves every
+// row's piece by itself: 128 experts of 1536 x 2048, 1500 tokens, float32: 442 us, 305 where the forms are in the cache already.
+// So the experts are taken in runs of kAheadExperts, and in front of a run's tiles some workgroups read the next run's
+// columns, a kilobyte and more of every row, into the cache that the XCDs share (through LDS, where nobody reads them): 358 us.
+// Runs of 16 and 32 gave 358 and 367 (4096 x 7168, 64 experts here: 1076, 1120 and 1196 for 8, 16 and 32); 4 leave XCDs
+// without patches.  32 workgroups that read ahead and 64 or 128: alike.
+constexpr int kAheadExperts = 8, kAheadBlocks = 32;
+__device__ __forceinline__ void columns_ahead(const ProductArgs &p, const GroupArgs &g, int e0, int index, uint8_t *lds) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64;
+    if (e0 >= g.n) return;
+    const int first = group_start(g, e0), bytes = group_start(g, min(e0 + kAheadExperts, g.n)) - first;   // a multiple of 128
+    if (bytes <= 0) return;
+    const uint32_t to = lds_address(lds) + wave * 1024;
+    for (int row = index * waves + wave; row < p.M + p.R; row += kAheadBlocks * waves) {
+        const uint8_t *from = (row < p.M ? p.a + static_cast<size_t>(row) * p.Kp : p.b + static_cast<size_t>(row - p.M) * p.Kp) + first;
+        for (int at = 0; at < bytes; at += 1024) dma16(from, min(at + 16 * lane_id(), bytes - 16), to);
+    }
+    wait_vmcnt<0>();
+}
+
+// Patches of up to 4 B tiles by all A tiles go over the XCDs in turn: groups of unlike sizes then keep all of them busy.  An
+// expert's patches are alike: 6 B tiles as 4 and 2 in place of 3 and 3 give some XCDs twice the work of others (64
+// experts of 1408 x 2048, mean 96 and 512 rows: 125 and 209 us, 105 and 173).
+__host__ __device__ __forceinline__ int grad_bands(int nb) { return (nb + 3) / 4; }
+
+template <int WA, int WB, int GA, int GB, bool WIDE, int OUT, bool AHEAD>
 __global__ __launch_bounds__(64 * GA * GB, 2) void expert_grad(ProductArgs p, GroupArgs g, int na, int nb) {
     constexpr int BA = 16 * WA * GA, BB = 16 * WB * GB;
-    // Patches of kBand B tiles by all A tiles go over the XCDs in turn: groups of unlike sizes then keep all of them busy.
-    constexpr int kBand = 4;
-    const int bands = (nb + kBand - 1) / kBand, i = blockIdx.x / 8, turn = i / (kBand * na), at = i - turn * (kBand * na);
-    const int patch = turn * 8 + blockIdx.x % 8, e = patch / bands, band = patch - e * bands, bw = min(kBand, nb - band * kBand);
-    if (e >= g.n || at >= bw * na) return;
-    const int ta = at / bw, tb = band * kBand + at % bw;
+    const int bands = grad_bands(nb), wide = (nb + bands - 1) / bands;
+    int block = blockIdx.x, e0 = 0, experts = g.n;
+    if constexpr (AHEAD) {
+        const int tiles = (kAheadExperts * bands + 7) / 8 * 8 * wide * na, run = block / (kAheadBlocks + tiles);
+        block -= run * (kAheadBlocks + tiles);
+        e0 = run * kAheadExperts;
+        experts = min(kAheadExperts, g.n - e0);
+        if (block < kAheadBlocks) {
+            __shared__ __attribute__((aligned(1024))) uint8_t nowhere[GA * GB * 1024];
+            columns_ahead(p, g, e0 + kAheadExperts, block, nowhere);
+            return;
+        }
+        block -= kAheadBlocks;
+    }
+    const int i = block / 8, turn = i / (wide * na), at = i - turn * (wide * na);
+    const int patch = turn * 8 + block % 8, of = patch / bands, band = patch - of * bands, bw = min(wide, nb - band * wide);
+    if (of >= experts || at >= bw * na) return;
+    const int e = e0 + of, ta = at / bw, tb = band * wide + at % bw;
     int o = 0, blocks = 0;   // without tables there are no rows
     if (g.off) {
         o = group_start(g, e);
@@ -183,20 +220,33 @@ hipError_t launch_expert_product(const ProductArgs &p, const GroupArgs &g, long 
 }
 
 template <int WA, int WB, int GA, int GB, bool WIDE, int OUT>
-static void grad(const ProductArgs &p, const GroupArgs &g, hipStream_t s) {
-    const int na = (p.M + 16 * WA * GA - 1) / (16 * WA * GA), nb = (p.R + 16 * WB * GB - 1) / (16 * WB * GB);
-    const int patches = g.n * ((nb + 3) / 4);
-    hipLaunchKernelGGL((expert_grad<WA, WB, GA, GB, WIDE, OUT>), dim3((patches + 7) / 8 * 8 * 4 * na), dim3(64 * GA * GB), 0, s, p, g, na, nb);
+static void grad(const ProductArgs &p, const GroupArgs &g, bool ahead, hipStream_t s) {
+    const int na = (p.M + 16 * WA * GA - 1) / (16 * WA * GA), nb = (p.R + 16 * WB * GB - 1) / (16 * WB * GB), bands = grad_bands(nb);
+    const int wide = (nb + bands - 1) / bands;
+    auto tiles = [&](int experts) { return (experts * bands + 7) / 8 * 8 * wide * na; };
+    if (ahead) {
+        const int runs = (g.n + kAheadExperts - 1) / kAheadExperts;
+        hipLaunchKernelGGL((expert_grad<WA, WB, GA, GB, WIDE, OUT, true>), dim3(runs * (kAheadBlocks + tiles(kAheadExperts))), dim3(64 * GA * GB), 0, s, p, g, na, nb);
+    } else {
+        hipLaunchKernelGGL((expert_grad<WA, WB, GA, GB, WIDE, OUT, false>), dim3(tiles(g.n)), dim3(64 * GA * GB), 0, s, p, g, na, nb);
+    }
 }
 
-// Short reductions want small tiles, whose loads and stores overlap between the two of a CU (128 x 128 against 256 x 256,
-// bf16, mean 4, 94, 256, 512 and 1024 rows: 220 190 588 415 224 and 256 240 556 386 217 us; 256 x 128 lies between them
-// or above).  float32 results, whose operands are widened in registers: 128 x 128 was best of 128 x 64, 256 x 64 and 256 x 128.
+// bf16: 256 x 256 where three rounds of the CUs are full or one nearly is, as one such tile of 1 to 64 steps reads half of
+// what four of 128 x 128 do (64 experts of 2048 x 1536, mean 16, 96, 512 and 1024 rows: 99 111 178 258 us, 128 x 128:
+// 118 131 202 294).  Fewer tiles leave CUs without work in the last round (64 of 512 x 768, mean 512 and 1024: 45 and
+// 76 us, 128 x 128: 43 and 62; 16 of 1024 x 1024, mean 1024: 49 and 42).  float32 results, whose operands are widened in registers:
+// 128 x 128 was best of 128 x 64, 256 x 64, 128 x 256 and 256 x 128 (128 of 1536 x 2048, mean 94: 417 us, the last two 432 and 467).
+// Reading ahead gains up to some 512 rows a group (32 of 4096 x 7168, mean 48, 256, 512 and 1024: 635 657 827 1151 us without,
+// 545 572 761 1144 with it) and from two runs of experts on (8 to 15 experts: alike, or slower).
 hipError_t launch_expert_weight_grad(const ProductArgs &p, const GroupArgs &g, float mean, int out, hipStream_t s) {
-    if (out == 0 && mean <= 192) grad<4, 4, 2, 2, false, 0>(p, g, s);
-    else if (out == 0) grad<8, 4, 2, 4, false, 0>(p, g, s);
-    else if (out == 1) grad<4, 4, 2, 2, true, 1>(p, g, s);
-    else grad<4, 4, 2, 2, true, 2>(p, g, s);
+    const bool ahead = g.off && g.n >= 2 * kAheadExperts && mean <= 1024;
+    const float largest = static_cast<float>((p.M + 255) / 256) * ((p.R + 255) / 256) * g.n;   // tiles of 256 x 256
+    const bool full = largest >= 768 || (largest > 128 && largest <= 224);
+    if (out == 0 && full) grad<8, 4, 2, 4, false, 0>(p, g, ahead, s);
+    else if (out == 0) grad<4, 4, 2, 2, false, 0>(p, g, ahead, s);
+    else if (out == 1) grad<4, 4, 2, 2, true, 1>(p, g, ahead, s);
+    else grad<4, 4, 2, 2, true, 2>(p, g, ahead, s);
     return hipGetLastError();
 }
 

@@ -463,6 +463,34 @@ def test_products_and_gradients_of_the_largest_tile(T, E, k, N, K):
     assert_product(dw, v, mag, int(want["count"].max()), BF16)
 
 
+@pytest.mark.parametrize("T,E,k,N,K", ((700, 16, 2, 272, 400), (300, 20, 2, 1040, 272), (60, 200, 2, 272, 272), (20, 1000, 1, 16, 32),
+                                       (9000, 16, 2, 48, 144), (40, 34, 1, 2064, 144), (200, 3, 1, 4112, 4112)))
+def test_weight_gradients_of_runs_of_experts(T, E, k, N, K):
+    """From 16 experts on their columns are read a run of experts ahead: whole and partial runs, runs without any row, bands of
+    one to three tiles, tables that leave the runs' order; and many tiles of few experts, which read nothing ahead."""
+    r = rng(T, E, N, K, 21)
+    skew = routing(r, T, E, k, 4.0)
+    d = desc(E, k, 128, T)
+    want = experts.sort(skew, 0, E, 128, d["rows"])
+    s, end = tables_of(want), int(want["off"][-1])
+    real = np.zeros((d["rows"], 1))
+    real[:end, 0] = want["row_pair"][:end] >= 0
+    dyv, xv = matrix(r, d["rows"], N, spread=1)[0] * real, matrix(r, d["rows"], K, spread=1)[0] * real
+    (dc, a), (xc, b) = form_of(dyv.T), form_of(xv.T)
+    dc.codes[:, end:], xc.codes[:, end:] = 0x7F, 0x7F
+    v, mag = experts.weight_grad(want, a.T, b.T)
+    most = max(1, int(want["count"].max()))
+    for dt in (BF16, F32):
+        dw = torch.full((E + 1, N, K), 3.0, dtype=TORCH[dt], device="cuda")
+        ftm.ft_expert_weight_grad(d, N, K, dc, xc, s, T, dw)
+        assert torch.all(dw[E] == 3.0)
+        assert_product(dw[:E], v, mag, most, dt)
+    if E >= 16:
+        s.off.copy_(s.off.flip(0))                              # every group ends before it starts
+        ftm.ft_expert_weight_grad(d, N, K, dc, xc, s, T, dw)
+        assert not dw[:E].any() and torch.all(dw[E] == 3.0)
+
+
 @pytest.mark.parametrize("T,E,k,N,K", ((2400, 16, 2, 4352, 272), (2000, 34, 3, 2048, 1040), (1300, 3, 1, 12544, 400)))
 def test_products_of_tall_tiles_and_blocks_of_scale_0(T, E, k, N, K):
     """Enough tiles for those of 256 x 128 and 256 x 256; weight blocks of scale 0 meet codes that are NaN."""
