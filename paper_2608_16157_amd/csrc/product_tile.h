@@ -261,16 +261,19 @@ __device__ __forceinline__ void again(const ProductArgs &p, int a0, int b0, int 
 // behind which the scale hides whole, draw more power: 206 us at the same busy share and a lower clock.
 // Tile at rows a0 of A and b0 of B, blocks [k0, k1), k1 > k0.  GROUPED: the rows from p.R up to `end` are stored as zeros.
 // STREAM: the results' stores do not stay in the caches.
+// lds: lds_tile_bytes, aligned to 1024.
+template <int WA, int WB, int GA, int GB>
+constexpr int lds_tile_bytes = 5 * 8 * WA * GA * 128 + 2 * 16 * WB * GB * 128 + 4 * 512;
+
 template <int WA, int WB, int GA, int GB, int ASC, bool WIDE, int OUT, bool GROUPED, bool STREAM>
-__device__ __forceinline__ void lds_tile(ProductArgs p, int a0, int b0, int k0, int k1, int end) {
+__device__ __forceinline__ void lds_tile(uint8_t *lds, ProductArgs p, int a0, int b0, int k0, int k1, int end) {
     constexpr bool kWide = WIDE;
     constexpr int NW = GA * GB, BA = 16 * WA * GA, BB = 16 * WB * GB, HS = WA / 2;   // HS steps per half
     constexpr int kHalf = BA / 2 * 128, kAHalves = 5, kBBlock = BB * 128;
     constexpr int kB = kAHalves * kHalf, kS = kB + 2 * kBBlock;     // LDS: A halves, B blocks, 4 blocks' scales
     constexpr int AH = BA / 2 / 8 / NW, BI = BB / 8 / NW;           // 1 KB requests per wave
     constexpr int kInFlight = 3 * AH + BI + 1;                      // younger than what a hand-off waits for
-    static_assert(AH * 16 * NW == BA && BI * 8 * NW == BB && BA <= 256 && BB <= 256 && WA % 2 == 0, "tile");
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[kS + 4 * 512];
+    static_assert(AH * 16 * NW == BA && BI * 8 * NW == BB && BA <= 256 && BB <= 256 && WA % 2 == 0 && kS + 4 * 512 == lds_tile_bytes<WA, WB, GA, GB>, "tile");
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = lane_id();
     const int r = lane & 15, g = lane >> 4, wa = wave % GA, wb = wave / GA;
     const int nkb = k1 - k0;   // blocks k0 .. k0 + nkb - 1 of the Kp / 128
@@ -487,7 +490,7 @@ __device__ __forceinline__ void lds_tile(ProductArgs p, int a0, int b0, int k0, 
     // Through LDS, 16 rows of B at a time and each wave by itself, so that whole lines leave: as the sums lie in
     // the registers, a store would write 32 bytes of each of 16 rows (8192 x 4096 results: 28 us for K = 128 against 21).
     constexpr int kSize = OUT == 0 ? 2 : 4, kRow = 16 * WA * kSize, kPitch = kRow + 16, kLanes = kRow / 16;
-    static_assert(16 * kPitch * NW <= sizeof(lds), "epilogue");
+    static_assert(16 * kPitch * NW <= kS + 4 * 512, "epilogue");
     stage_barrier();   // every wave has read its last operands, and its requests have landed
     // A weight block with scale 0 adds nothing, whatever its codes and the rows that meet them hold.  Where those are
     // finite its product was 0 already; where a sum is NaN the wave forms its sums again without such blocks, in the
@@ -555,7 +558,8 @@ __global__ __launch_bounds__(64 * GA * GB, 2) void product_tiled(ProductArgs p, 
     int ta, tb, k0, k1;
     tile_at(xcd_remap(blockIdx.x, na * nb), na, nb, ta, tb);
     split_range(p, p.Kp / 128, k0, k1);
-    lds_tile<WA, WB, GA, GB, ASC, WIDE, OUT, false, false>(p, ta * 16 * WA * GA, tb * 16 * WB * GB, k0, k1, 0);
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[lds_tile_bytes<WA, WB, GA, GB>];
+    lds_tile<WA, WB, GA, GB, ASC, WIDE, OUT, false, false>(lds, p, ta * 16 * WA * GA, tb * 16 * WB * GB, k0, k1, 0);
 }
 
 }  // namespace ftmoe

@@ -515,6 +515,23 @@ def test_products_of_tall_tiles_and_blocks_of_scale_0(T, E, k, N, K):
     assert torch.equal(torch.isnan(y[:end]).any(dim=1), real) and torch.all(y[end:] == 7.0)
 
 
+@pytest.mark.parametrize("align", (16, 128))
+@pytest.mark.parametrize("T,E,k,N,K", ((500, 3, 3, 12416, 144), (560, 3, 3, 12432, 16), (225, 9, 2, 8176, 144), (90, 9, 5, 8080, 272),
+                                       (1500, 3, 1, 16400, 48)))
+def test_products_whose_last_round_is_halved(T, E, k, N, K, align):
+    """Some tiles more than a multiple of the CUs: tiles of half the features, whose second half may be 16 rows or none."""
+    r = rng(T, E, N, K, 22)
+    wt, w = expert_weights(r, E, N, K)
+    d, want, s = layout(r, T, E, k, align)
+    form, q = form_of(matrix(r, d["rows"], K, spread=1)[0])
+    end = int(want["off"][-1])
+    y = run_experts(d, s, wt, form, N, K, T, BF16)
+    v, mag = experts.product(want, q, w)
+    assert_product(y[:end], v, mag, K, BF16)
+    assert torch.all(y[end:] == 7.0)
+    assert not y[:end][cuda(want["row_pair"][:end] < 0)].any()
+
+
 @pytest.mark.parametrize("T,E,k", ((40, 63, 3), (40, 64, 3), (40, 65, 3), (200, 1000, 4), (3000, 1024, 2)))
 def test_many_groups(T, E, k):
     """More groups than lanes: a workgroup finds its tile among them; tables with a bool mask, and with too few rows."""
