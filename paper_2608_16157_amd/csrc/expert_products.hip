@@ -215,8 +215,9 @@ static void direct(const ProductArgs &p, const GroupArgs &g, long pairs, hipStre
 // 256 x 128, 256 x 256 (us):
 //   128 experts of 1536 x 2048, bf16    mean 1: 43.8 46.5 47.9 - 70.6;  4: 69.4 75.7 79.9 - 110;  8: 84.9 82.3 85.8 - 113;
 //                                       32: 169 89.7 93.6 - 140;  64: 333 126 109 104 132;  128: - 153 125 121 138
-//   64 of 1536 x 2048, bf16             256: - 119 93.1 91.1 98.6;  384: - - 135 121 124;  512: - 200 155 152 137
-//   32 of 2048 x 7168, bf16             192: - - 171 154 191;  256: - 241 192 176 196;  512: - 382 296 283 267
+//   64 of 1536 x 2048, bf16             192: - - 80.7 78.0 88.0;  256: - - 95.3 91.6 91.3;  320: - - 110 109 104;  384: - - 126 121 110
+//   32 of 4096 x 2048, bf16             192: - - 104 102 103;  256: - - 120 121 110;  384: - - 169 166 144;  1024: - - 370 354 310
+//   32 of 2048 x 7168, bf16             192: - - 175 158 169;  256: - - 203 190 195;  320: - - 235 212 212;  512: - - 339 313 275
 //   128 of 1536 x 2048, float32         mean 1: 45.1 52.1 63.2;  4: 73.5 84.7 103;  16: 112 97.8 117;  64: 336 151 142 151
 // Where the tiles of 128 x 128 fill the card no more than twice, or are odd in number along the features, the larger ones lose:
 // 8 of 576 x 4096, mean 1024: 34.1 50.9 49.6; 16 of 400 x 1040, mean 64: 10.8 13.5 18.8.  Direct tiles of 16 x 16, 16 x 32,
@@ -233,7 +234,7 @@ static hipError_t product(const ProductArgs &p, const GroupArgs &g, long pairs, 
     } else if constexpr (WIDE) {
         tiled<4, 4, 2, 2, WIDE, OUT>(p, g, pairs, s);
     } else {
-        if (mean > 384 && largest >= 192) tiled<8, 4, 2, 4, WIDE, OUT>(p, g, pairs, s);
+        if (mean >= 256 && largest >= 192) tiled<8, 4, 2, 4, WIDE, OUT>(p, g, pairs, s);
         else if (a128 % 2 == 0 && small >= 512) tiled<4, 4, 4, 2, WIDE, OUT>(p, g, pairs, s);
         else tiled<4, 4, 2, 2, WIDE, OUT>(p, g, pairs, s);
     }
