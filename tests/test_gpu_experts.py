@@ -516,7 +516,7 @@ def test_products_of_tall_tiles_and_blocks_of_scale_0(T, E, k, N, K):
 
 
 @pytest.mark.parametrize("align", (16, 128))
-@pytest.mark.parametrize("T,E,k,N,K", ((500, 3, 3, 12416, 144), (560, 3, 3, 12432, 16), (225, 9, 2, 8176, 144), (90, 9, 5, 8080, 272),
+@pytest.mark.parametrize("T,E,k,N,K", ((500, 3, 3, 12416, 144), (560, 3, 3, 12432, 16), (400, 3, 3, 12416, 144), (225, 9, 2, 8176, 144), (90, 9, 5, 8080, 272),
                                        (1500, 3, 1, 16400, 48)))
 def test_products_whose_last_round_is_halved(T, E, k, N, K, align):
     """Some tiles more than a multiple of the CUs: tiles of half the features, whose second half may be 16 rows or none."""
