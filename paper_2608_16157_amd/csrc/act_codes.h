@@ -117,12 +117,12 @@ __device__ __forceinline__ uint32_t mag_of(const float *v) {
 
 // a block's 128 values: 8 in each of the 16 lanes of a lane row, or 16 in each of the 8 lanes of half of one
 __device__ __forceinline__ uint32_t block_mag16(const float *v) { return row_max_u32(mag_of<8>(v)); }
-__device__ __forceinline__ uint32_t block_mag8(const float *v) {
-    uint32_t m = mag_of<16>(v);
+__device__ __forceinline__ uint32_t eight_max_u32(uint32_t m) {
     m = max(m, dpp_u32<0xB1>(m));       // quad_perm: lane ^ 1
     m = max(m, dpp_u32<0x4E>(m));       // quad_perm: lane ^ 2
     return max(m, dpp_u32<0x141>(m));   // row_half_mirror: 7 - lane
 }
+__device__ __forceinline__ uint32_t block_mag8(const float *v) { return eight_max_u32(mag_of<16>(v)); }
 
 // float32 -> bf16, round to nearest even; NaN stays NaN
 __device__ __forceinline__ uint32_t f32_to_bf16_any(float f) {

@@ -2,9 +2,10 @@
 // gradient of the gates (ft_expert_gate_grad).  row_pair and pair_row come from sort.hip; what lies outside their
 // ranges counts as no pair and no row.
 //
-// All of these move memory and compute little: the bound is HBM, and for the gather the L2, from which a row is read as often
-// as the token has experts.  8192 tokens of 7168 channels, 8 experts each (62000 to 65536 rows, 78000 to 82000 with padding): both forms
-// 277 us, the row form 205, plain rows 285; back to the tokens 204 us, 5.1 TB/s; the gates 190.
+// All of these move memory and compute little: the bound is HBM, and for the 8-bit forms the vector units, where a value is
+// handled in its own register (float32, weights); bf16 rows without weights are handled in pairs.  8192 tokens of 7168 channels, 8
+// experts each (62000 to 65536 rows, 78000 to 82000 with padding), replayed over buffers that no cache holds: both forms 270 us, 4.6 TB/s, the row form
+// 190, plain rows 285; back to the tokens 204 us, 5.1 TB/s; the gates 190.
 #include "act_tile.h"
 #include "gemm_tile.h"
 
@@ -19,15 +20,28 @@ __device__ __forceinline__ int row_token(const RowsArgs &a, long row, float &w) 
     w = 1.0f;
     if (static_cast<uint32_t>(p) >= static_cast<uint32_t>(a.T) * static_cast<uint32_t>(a.k)) return -1;
     if (a.w) w = a.w[p];
-    return p / a.k;
+    return a.over_k ? __umulhi(p, a.over_k) : p;
+}
+// The same of four rows in every lane of a lane row: each lane asks for one of them.
+__device__ __forceinline__ void row_tokens4(const RowsArgs &a, int row0, int sub, int (&t)[4], float (&w)[4]) {
+    float one;
+    const uint32_t mine = row_token(a, row0 + sub % 4, one), f = __float_as_uint(one);
+    t[0] = dpp_u32<kDppRowCopy0>(mine);
+    t[1] = dpp_u32<kDppRowCopy0 + 1>(mine);
+    t[2] = dpp_u32<kDppRowCopy0 + 2>(mine);
+    t[3] = dpp_u32<kDppRowCopy0 + 3>(mine);
+    w[0] = __uint_as_float(dpp_u32<kDppRowCopy0>(f));
+    w[1] = __uint_as_float(dpp_u32<kDppRowCopy0 + 1>(f));
+    w[2] = __uint_as_float(dpp_u32<kDppRowCopy0 + 2>(f));
+    w[3] = __uint_as_float(dpp_u32<kDppRowCopy0 + 3>(f));
 }
 // one past the last group's rows
 __device__ __forceinline__ int rows_end(const RowsArgs &a) { return min(a.off[a.n], a.rows); }
 
 // Block of 128 columns and block of `rows` rows of a workgroup, the columns outermost: what runs together on an XCD then
 // reads the same columns, of all tokens (2 MB of 8192 in bf16), and each is read from memory once however many rows want
-// it (both forms of 8192 x 7168, 8 experts a token, with the sort: 347 us; two, four and eight blocks of columns side by side 363, 370, 361;
-// rows outermost 440).  False past the groups' rows.
+// it (both forms of 8192 x 7168, 8 experts a token, with the sort, one value a register: 347 us; two, four and eight blocks of columns side by
+// side 363, 370, 361; rows outermost 440).  False past the groups' rows.
 __device__ __forceinline__ bool gather_place(const RowsArgs &a, int rows, int &cb, int &rb, int &end) {
     end = rows_end(a);
     const int nkb = (a.C + 127) / 128, nrb = (end + rows - 1) / rows;
@@ -75,12 +89,47 @@ __global__ __launch_bounds__(256) void gather_rows(RowsArgs a, const XT *x, ActF
     for (int r = 0; r < 2; ++r) load16(x + static_cast<size_t>(max(t[r], 0)) * a.C + min(c, a.C - 16), v[r]);
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-        quiet(v[r]);
-        if (a.w)
+        if (a.w)   // products are quiet
 #pragma unroll
             for (int q = 0; q < 16; ++q) v[r][q] *= w[r];
+        else quiet(v[r]);
         zero_unless(t[r] >= 0 && c < a.C, v[r]);   // C is a multiple of 16
         if (row0 + 32 * r < end) put_row<true>(v[r], f, row0 + 32 * r, end, kb, sub);
+    }
+}
+
+// The same of bf16 rows without weights.
+__global__ __launch_bounds__(256) void gather_rows_pairs(RowsArgs a, const uint16_t *x, ActForm f) {
+    int kb, rb, end;
+    if (!gather_place(a, 64, kb, rb, end)) return;
+    const int sub = threadIdx.x % 8, c = kb * 128 + 16 * sub, g = threadIdx.x / 8, row0 = rb * 64;
+    float none;
+    int t[2];
+    uint32_t w[2][8];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) t[r] = row_token(a, min(row0 + g + 32 * r, end - 1), none);
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint4 q = *reinterpret_cast<const uint4 *>(x + static_cast<size_t>(max(t[r], 0)) * a.C + min(c, a.C - 16) + 8 * i);
+            w[r][4 * i] = q.x;
+            w[r][4 * i + 1] = q.y;
+            w[r][4 * i + 2] = q.z;
+            w[r][4 * i + 3] = q.w;
+        }
+    uint8_t *codes = f.codes + static_cast<size_t>(row0) * f.Kp + kb * 128, *scales = f.scales + static_cast<size_t>(kb) * f.Rp + row0;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[r][i] = t[r] >= 0 && c < a.C ? w[r][i] : 0u;
+        const int row = g + 32 * r, byte = act_scale_byte(eight_max_u32(mag_of_pairs(w[r])));
+        const float sc = act_scale_operand(byte);
+        if (row0 + row >= end) continue;
+        put_words<true>(codes + (static_cast<uint32_t>(row) * f.Kp + 16 * sub),
+                        u32x4_t{act_codes4_bf16(w[r][0], w[r][1], sc, 0), act_codes4_bf16(w[r][2], w[r][3], sc, 0),
+                                act_codes4_bf16(w[r][4], w[r][5], sc, 0), act_codes4_bf16(w[r][6], w[r][7], sc, 0)});
+        if (sub == 0) scales[row] = static_cast<uint8_t>(byte);
     }
 }
 
@@ -94,20 +143,46 @@ __global__ __launch_bounds__(kActThreads) void gather_tiles(RowsArgs a, const XT
     const int row0 = rb * 128 + kActRows * g, c = cb * 128 + 8 * sub;
     float v[1][kActRows][8], w[kActRows];
     int t[kActRows];
-#pragma unroll
-    for (int r = 0; r < kActRows; ++r) t[r] = row_token(a, row0 + r, w[r]);
+    row_tokens4(a, row0, sub, t, w);
 #pragma unroll
     for (int r = 0; r < kActRows; ++r) load8(x + static_cast<size_t>(max(t[r], 0)) * a.C + min(c, a.C - 8), v[0][r]);
 #pragma unroll
     for (int r = 0; r < kActRows; ++r) {
-        quiet(v[0][r]);
-        if (a.w)
+        if (a.w)   // products are quiet
 #pragma unroll
             for (int q = 0; q < 8; ++q) v[0][r][q] *= w[r];
+        else quiet(v[0][r]);
         zero_unless(t[r] >= 0 && c < a.C, v[0][r]);   // C is a multiple of 16
     }
     const ActPlane to[1] = {{row, cb, col, cb * 128}};
     put_tile<1, true>(v, sh, to, rb * 128, rb);
+}
+
+// The same of bf16 rows without weights.
+__global__ __launch_bounds__(kActThreads) void gather_tiles_pairs(RowsArgs a, const uint16_t *x, ActForm row, ActForm col) {
+    __shared__ __attribute__((aligned(16))) PairTileShared sh;
+    const int g = threadIdx.x / 16, sub = threadIdx.x % 16;
+    int cb, rb, end;
+    if (!gather_place(a, 128, cb, rb, end)) return;
+    const int c = cb * 128 + 8 * sub;
+    int t[kActRows];
+    float none[kActRows];
+    row_tokens4(a, rb * 128 + kActRows * g, sub, t, none);
+    uint32_t w[kActRows][4];
+#pragma unroll
+    for (int r = 0; r < kActRows; ++r) {
+        const uint4 q = *reinterpret_cast<const uint4 *>(x + static_cast<size_t>(max(t[r], 0)) * a.C + min(c, a.C - 8));
+        w[r][0] = q.x;
+        w[r][1] = q.y;
+        w[r][2] = q.z;
+        w[r][3] = q.w;
+    }
+    if (__ballot((t[0] | t[1] | t[2] | t[3]) >= 0 && c < a.C) != ~0ull)   // C is a multiple of 16
+#pragma unroll
+        for (int r = 0; r < kActRows; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[r][i] = t[r] >= 0 && c < a.C ? w[r][i] : 0u;
+    put_tile_pairs<true>(w, sh, ActPlane{row, cb, col, cb * 128}, rb * 128, rb);
 }
 
 template <class XT>
@@ -121,6 +196,14 @@ static void gather(const RowsArgs &a, const XT *x, void *plain, bool plain_f32, 
             hipLaunchKernelGGL((gather_plain<XT, uint16_t>), grid, dim3(256), 0, s, a, x, static_cast<uint16_t *>(plain));
     }
     const unsigned nkb = (a.C + 127) / 128;
+    if constexpr (std::is_same_v<XT, uint16_t>)
+        if (!a.w) {
+            if (col.codes)
+                hipLaunchKernelGGL(gather_tiles_pairs, dim3(nkb * (a.rows / 128)), dim3(kActThreads), 0, s, a, x, row, col);
+            else if (row.codes)
+                hipLaunchKernelGGL(gather_rows_pairs, dim3(nkb * ((a.rows + 63) / 64)), dim3(256), 0, s, a, x, row);
+            return;
+        }
     if (col.codes)
         hipLaunchKernelGGL(gather_tiles<XT>, dim3(nkb * (a.rows / 128)), dim3(kActThreads), 0, s, a, x, row, col);
     else if (row.codes)

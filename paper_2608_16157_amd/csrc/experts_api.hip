@@ -73,7 +73,9 @@ SortWs sort_ws(const ft_sort_desc_t *d, int T) {
 }
 
 RowsArgs rows_args(const ft_sort_desc_t *d, const ft_sort_t *t, int T, int C, const float *w) {
-    return RowsArgs{t->row_pair, t->pair_row, t->off, w, T, d->top_k, d->local, d->rows, C};
+    // a pair's token: pairs are below 2^20 k and k at most 64, so that pair * k < 2^32 and the product's high word is exact
+    const uint32_t over_k = d->top_k > 1 ? static_cast<uint32_t>((1ull << 32) / d->top_k + 1) : 0;
+    return RowsArgs{t->row_pair, t->pair_row, t->off, w, T, d->top_k, d->local, d->rows, C, over_k};
 }
 
 GroupArgs group_args(const ft_sort_desc_t *d, const ft_sort_t *t) {

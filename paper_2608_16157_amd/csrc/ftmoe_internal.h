@@ -100,6 +100,7 @@ struct RowsArgs {
     const int32_t *row_pair, *pair_row, *off;
     const float *w;         // [T][k] or null
     int T, k, n, rows, C;
+    uint32_t over_k;        // floor(2^32 / k) + 1; 0 for k = 1
 };
 
 // Groups of rows, one per expert, for a product (expert_products.hip).

@@ -260,6 +260,34 @@ def test_rows_that_are_not_finite():
             assert np.allclose(got[t], here * x[t] if here else 0.0, rtol=1e-6, equal_nan=True)
 
 
+@pytest.mark.parametrize("align", (16, 128))
+@pytest.mark.parametrize("order", ("as they come", "mixed", "by magnitude"))
+def test_gather_of_every_bf16_value(order, align):
+    """bf16 rows go to 8 bits two values at a time: the same forms as of the values in float32, every bit pattern among them
+    (signed zeros, subnormals, infinities, quiet and signalling NaNs of both signs), but for the masked tokens'."""
+    r, T, C, k = rng(len(order), align), 128, 512, 3
+    bits = np.arange(65536, dtype=np.uint16)
+    if order == "mixed":
+        bits = r.permutation(bits)
+    elif order == "by magnitude":
+        bits = np.concatenate([bits[:32768], bits[32768:]]).reshape(2, 32768).T.reshape(-1)
+    x = cuda(bits.view(np.int16).reshape(T, C)).view(torch.bfloat16)
+    wide = torch.from_numpy((bits.astype(np.uint32) << 16).view(np.float32).reshape(T, C)).cuda()
+    d, want, s = layout(r, T, 5, k, align)
+    end = int(want["off"][-1])
+    both = align == 128
+    got, ref = ([filled(d["rows"], C)] + [filled(C, d["rows"])] * both for _ in range(2))
+    for xs, forms in ((x, got), (wide, ref)):
+        ftm.ft_expert_gather(d, s, xs, T, C, row=forms[0], col=forms[1] if both else None)
+    token = np.where(want["row_pair"][:end] >= 0, want["row_pair"][:end] // k, 0)
+    bad = ~torch.isfinite(wide)[cuda(token)] & cuda(want["row_pair"][:end] >= 0)[:, None]
+    for i, (a, b) in enumerate(zip(got, ref)):
+        p, q, nan = (a.codes[:end], b.codes[:end], bad) if i == 0 else (a.codes[:, :end], b.codes[:, :end], bad.T)
+        assert torch.equal(a.scales, b.scales)
+        assert torch.equal(p[~nan], q[~nan])
+        assert torch.all((p[nan] & 0x7F) == 0x7F) and torch.all((q[nan] & 0x7F) == 0x7F)
+
+
 @pytest.mark.parametrize("rt,yt", ((BF16, BF16), (F32, F32), (BF16, F32), (F32, BF16)))
 @pytest.mark.parametrize("T,E,k,C", ROWS)
 def test_combine_and_gate_gradient(T, E, k, C, rt, yt):
