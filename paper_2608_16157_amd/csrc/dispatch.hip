@@ -272,54 +272,78 @@ hipError_t launch_combine(const RowsArgs &a, const void *rows, bool rows_f32, co
     return hipGetLastError();
 }
 
-// d_w[t][j] = <dy[t], rows[row of (t, j)]>, 0 without a row.  A workgroup of four waves per token, each every fourth
-// run of 512 channels; sums of a lane, of a wave and of the waves in a fixed order.
-template <class RT, class YT>
+// d_w[t][j] = <dy[t], rows[row of (t, j)]>, 0 without a row.  WAVES waves per token, each every WAVES-th run of 512
+// channels; sums of a lane, of a wave and of the waves in a fixed order.  A lane looks one pair up, and only pairs with a row are
+// read, in lots of 8, 4, 2 and 1 (a lot past the last one reads it again: 6 of 8, 3 of 4).
+//
+// One wave a token where tokens are many and small: 30000 x 2 of 512 channels 18.9 us, four waves 41.8; 41261 x 1 of 3968, one in eight
+// here, 26.9 and 37.3; 8192 x 8 of 512, 15.5 and 18.9; of 1024 alike.  Four where not: 300 x 4 of 4096, 7.7 and 5.9; 4096 x 8 of
+// 4096, 67 and 63.  Eight loads for every eight pairs, with a row or without: 30000 x 2 82 us, 41261 x 1 228, 1500 x 8 of 2048 15.0
+// in place of 12.7.
+template <class RT, class YT, int WAVES>
 __global__ __launch_bounds__(256) void gate_grad(RowsArgs a, const RT *rows, const YT *dy, float *d_w) {
-    __shared__ float part[4][kPairsOnWay];
-    const int t = blockIdx.x, wave = threadIdx.x / 64, lane = lane_id();
-    const int32_t *at = a.pair_row + static_cast<size_t>(t) * a.k;
+    __shared__ float part[WAVES][kMaxTopK];
+    const int all = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wave = all % WAVES, lane = lane_id();
+    const int t = blockIdx.x * (4 / WAVES) + all / WAVES;
+    if (t >= a.T) return;   // waves that meet no barrier
     const YT *d = dy + static_cast<size_t>(t) * a.C;
-    for (int j0 = 0; j0 < a.k; j0 += kPairsOnWay) {
-        const RT *from[kPairsOnWay];
-        bool in[kPairsOnWay];
-        float sum[kPairsOnWay];
+    const int row = lane < a.k ? a.pair_row[static_cast<size_t>(t) * a.k + lane] : -1;
+    uint64_t left = __ballot(static_cast<uint32_t>(row) < static_cast<uint32_t>(a.rows));
+    float mine = 0.0f;   // of pair `lane`, over this wave's channels
+    auto lot = [&](auto n) {
+        constexpr int P = decltype(n)::value;
+        const RT *from[P];
+        int pair[P];
+        float sum[P];
 #pragma unroll
-        for (int j = 0; j < kPairsOnWay; ++j) {
-            const int row = at[min(j0 + j, a.k - 1)];
-            in[j] = j0 + j < a.k && static_cast<uint32_t>(row) < static_cast<uint32_t>(a.rows);
-            from[j] = rows + static_cast<size_t>(in[j] ? row : 0) * a.C;
+        for (int j = 0; j < P; ++j) {
+            pair[j] = left ? __builtin_ctzll(left) : pair[max(j - 1, 0)];
+            left &= left - 1;
+            from[j] = rows + static_cast<size_t>(readlane_u32(row, pair[j])) * a.C;
             sum[j] = 0.0f;
         }
-        for (int c = 512 * wave + 8 * lane; c < a.C; c += 2048) {
-            float g[8], v[kPairsOnWay][8];
+        for (int c = 512 * wave + 8 * lane; c < a.C; c += 512 * WAVES) {
+            float g[8], v[P][8];
             load8(d + c, g);
 #pragma unroll
-            for (int j = 0; j < kPairsOnWay; ++j) load8(from[j] + c, v[j]);
+            for (int j = 0; j < P; ++j) load8(from[j] + c, v[j]);
 #pragma unroll
-            for (int j = 0; j < kPairsOnWay; ++j)
+            for (int j = 0; j < P; ++j)
 #pragma unroll
                 for (int q = 0; q < 8; ++q) sum[j] = fmaf(g[q], v[j][q], sum[j]);
         }
 #pragma unroll
-        for (int j = 0; j < kPairsOnWay; ++j) sum[j] = wave_sum_f32(sum[j]);
-        __syncthreads();   // the last pairs' parts have been read
-        if (lane == 0)
-#pragma unroll
-            for (int j = 0; j < kPairsOnWay; ++j) part[wave][j] = in[j] ? sum[j] : 0.0f;
-        __syncthreads();
-        const int j = threadIdx.x;
-        if (j < kPairsOnWay && j0 + j < a.k)
-            d_w[static_cast<size_t>(t) * a.k + j0 + j] = (part[0][j] + part[1][j]) + (part[2][j] + part[3][j]);
+        for (int j = 0; j < P; ++j) {
+            const float whole = wave_sum_f32(sum[j]);
+            mine = lane == pair[j] ? whole : mine;
+        }
+    };
+    while (left) {
+        const int n = __popcll(left);
+        if (n >= 6) lot(std::integral_constant<int, 8>{});
+        else if (n >= 3) lot(std::integral_constant<int, 4>{});
+        else if (n == 2) lot(std::integral_constant<int, 2>{});
+        else lot(std::integral_constant<int, 1>{});
     }
+    if constexpr (WAVES > 1) {
+        part[wave][lane] = mine;
+        __syncthreads();
+        if (wave > 0) return;
+        mine = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
+    }
+    if (lane < a.k) d_w[static_cast<size_t>(t) * a.k + lane] = mine;
 }
 
 hipError_t launch_gate_grad(const RowsArgs &a, const void *rows, bool rows_f32, const void *dy, bool dy_f32, float *d_w, hipStream_t s) {
     auto go = [&](auto *r, auto *o) {
         using RT = std::remove_pointer_t<decltype(r)>;
         using YT = std::remove_pointer_t<decltype(o)>;
-        hipLaunchKernelGGL((gate_grad<RT, YT>), dim3(a.T), dim3(256), 0, s, a, static_cast<const RT *>(rows),
-                           static_cast<const YT *>(dy), d_w);
+        if (a.T >= 2048 && a.C * a.k <= 8192)
+            hipLaunchKernelGGL((gate_grad<RT, YT, 1>), dim3((a.T + 3) / 4), dim3(256), 0, s, a, static_cast<const RT *>(rows),
+                               static_cast<const YT *>(dy), d_w);
+        else
+            hipLaunchKernelGGL((gate_grad<RT, YT, 4>), dim3(a.T), dim3(256), 0, s, a, static_cast<const RT *>(rows),
+                               static_cast<const YT *>(dy), d_w);
     };
     float *f = nullptr;
     uint16_t *h = nullptr;

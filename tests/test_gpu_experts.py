@@ -319,6 +319,25 @@ def test_combine_and_gate_gradient(T, E, k, C, rt, yt):
     assert np.all(f64(d_w[:T])[want["pair_row"] < 0] == 0)
 
 
+@pytest.mark.parametrize("rt,yt", ((BF16, BF16), (F32, F32), (BF16, F32)))
+@pytest.mark.parametrize("T,E,k,C", ((2047, 4, 3, 80), (2048, 4, 3, 80), (2049, 20, 1, 8192), (2050, 20, 7, 1040), (2051, 64, 64, 128),
+                                     (2303, 66, 9, 528), (2100, 8, 4, 2064)))
+def test_gate_gradient_of_many_tokens(T, E, k, C, rt, yt):
+    """One wave a token, and the sizes beside it; pairs of which all, some or none have a row, in lots of every size."""
+    r = rng(T, E, C, rt, yt, 23)
+    d, want, s = layout(r, T, E, k, 16, part=E >= 20)
+    rv, rows = matrix(r, d["rows"], C, rt, spread=1)
+    rows[int(want["off"][-1]):] = float("nan")      # behind the last group: not read
+    dv, dy = matrix(r, T, C, yt, spread=1)
+    none = want["pair_row"].max(axis=1) < 0
+    dy[cuda(none)] = float("nan")                   # tokens without rows: zeros whatever they hold
+    d_w = torch.full((T + 1, k), 5.0, device="cuda")
+    ftm.ft_expert_gate_grad(d, s, rows, dy, T, C, d_w)
+    v, mag = experts.gate_grad(want, rv, dv)
+    assert np.all(np.abs(f64(d_w[:T]) - v) <= max(C, 24) * U * mag) and torch.all(d_w[T] == 5.0)
+    assert np.all(f64(d_w[:T])[want["pair_row"] < 0] == 0)
+
+
 def test_tables_out_of_range_are_no_pairs_and_no_rows():
     T, E, k, C = 4, 3, 2, 144
     d = desc(E, k, 16, T)
