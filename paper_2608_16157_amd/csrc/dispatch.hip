@@ -42,9 +42,9 @@ __device__ __forceinline__ int rows_end(const RowsArgs &a) { return min(a.off[a.
 // reads the same columns, of all tokens (2 MB of 8192 in bf16), and each is read from memory once however many rows want
 // it (both forms of 8192 x 7168, 8 experts a token, with the sort, one value a register: 347 us; two, four and eight blocks of columns side by
 // side 363, 370, 361; rows outermost 440).  False past the groups' rows.
-__device__ __forceinline__ bool gather_place(const RowsArgs &a, int rows, int &cb, int &rb, int &end) {
+__device__ __forceinline__ bool gather_place(const RowsArgs &a, int columns, int rows, int &cb, int &rb, int &end) {
     end = rows_end(a);
-    const int nkb = (a.C + 127) / 128, nrb = (end + rows - 1) / rows;
+    const int nkb = (columns + 127) / 128, nrb = (end + rows - 1) / rows;
     if (end <= 0 || static_cast<long>(blockIdx.x) >= static_cast<long>(nkb) * nrb) return false;
     const int L = xcd_remap(blockIdx.x, nkb * nrb);
     cb = L / nrb;
@@ -52,25 +52,35 @@ __device__ __forceinline__ bool gather_place(const RowsArgs &a, int rows, int &c
     return true;
 }
 
-// Plain rows: 16 lanes per (row, block of 128), four rows on the way at once.
+// Plain rows: 16 lanes per (row, block of 128), four rows on the way at once.  Where rows are not whole lines of 128 bytes a
+// row's blocks begin as many columns before it as its start lies behind a line's, so that stores are whole lines all the same
+// (2000 x 8 of 7376 channels bf16, with the sort: 72 us; blocks from the row's start on, which straddle lines, 128).
+template <class OT>
+__host__ __device__ constexpr int plain_columns(int C) {
+    constexpr int kLine = 128 / sizeof(OT);
+    return C % kLine == 0 ? C : C + kLine - 16;   // C is a multiple of 16
+}
 template <class XT, class OT>
 __global__ __launch_bounds__(256) void gather_plain(RowsArgs a, const XT *x, OT *out) {
     int cb, rb, end;
-    if (!gather_place(a, 64, cb, rb, end)) return;
-    const int c = cb * 128 + 8 * (threadIdx.x % 16), row0 = rb * 64 + threadIdx.x / 16;
+    if (!gather_place(a, plain_columns<OT>(a.C), 64, cb, rb, end)) return;
+    const int row0 = rb * 64 + threadIdx.x / 16;
     float v[4][8], w[4];
-    int t[4];
+    int t[4], c[4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) t[r] = row_token(a, min(row0 + 16 * r, end - 1), w[r]);
+    for (int r = 0; r < 4; ++r) {
+        c[r] = cb * 128 + 8 * static_cast<int>(threadIdx.x % 16) - static_cast<int>(static_cast<uint32_t>(row0 + 16 * r) * a.C % (128 / sizeof(OT)));
+        t[r] = row_token(a, min(row0 + 16 * r, end - 1), w[r]);
+    }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) load8(x + static_cast<size_t>(max(t[r], 0)) * a.C + min(c, a.C - 8), v[r]);
+    for (int r = 0; r < 4; ++r) load8(x + static_cast<size_t>(max(t[r], 0)) * a.C + min(max(c[r], 0), a.C - 8), v[r]);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         if (a.w)
 #pragma unroll
             for (int q = 0; q < 8; ++q) v[r][q] *= w[r];
         zero_unless(t[r] >= 0, v[r]);
-        if (row0 + 16 * r < end && c < a.C) store8<true>(out + static_cast<size_t>(row0 + 16 * r) * a.C + c, v[r]);
+        if (row0 + 16 * r < end && c[r] >= 0 && c[r] < a.C) store8<true>(out + static_cast<size_t>(row0 + 16 * r) * a.C + c[r], v[r]);
     }
 }
 
@@ -78,7 +88,7 @@ __global__ __launch_bounds__(256) void gather_plain(RowsArgs a, const XT *x, OT 
 template <class XT>
 __global__ __launch_bounds__(256) void gather_rows(RowsArgs a, const XT *x, ActForm f) {
     int kb, rb, end;
-    if (!gather_place(a, 64, kb, rb, end)) return;
+    if (!gather_place(a, a.C, 64, kb, rb, end)) return;
     const int sub = threadIdx.x % 8, c = kb * 128 + 16 * sub;
     const long row0 = rb * 64L + threadIdx.x / 8;
     float v[2][16], w[2];
@@ -101,7 +111,7 @@ __global__ __launch_bounds__(256) void gather_rows(RowsArgs a, const XT *x, ActF
 // The same of bf16 rows without weights.
 __global__ __launch_bounds__(256) void gather_rows_pairs(RowsArgs a, const uint16_t *x, ActForm f) {
     int kb, rb, end;
-    if (!gather_place(a, 64, kb, rb, end)) return;
+    if (!gather_place(a, a.C, 64, kb, rb, end)) return;
     const int sub = threadIdx.x % 8, c = kb * 128 + 16 * sub, g = threadIdx.x / 8, row0 = rb * 64;
     float none;
     int t[2];
@@ -139,7 +149,7 @@ __global__ __launch_bounds__(kActThreads) void gather_tiles(RowsArgs a, const XT
     __shared__ __attribute__((aligned(16))) ActTileShared<1> sh;
     const int g = threadIdx.x / 16, sub = threadIdx.x % 16;
     int cb, rb, end;
-    if (!gather_place(a, 128, cb, rb, end)) return;
+    if (!gather_place(a, a.C, 128, cb, rb, end)) return;
     const int row0 = rb * 128 + kActRows * g, c = cb * 128 + 8 * sub;
     float v[1][kActRows][8], w[kActRows];
     int t[kActRows];
@@ -163,7 +173,7 @@ __global__ __launch_bounds__(kActThreads) void gather_tiles_pairs(RowsArgs a, co
     __shared__ __attribute__((aligned(16))) PairTileShared sh;
     const int g = threadIdx.x / 16, sub = threadIdx.x % 16;
     int cb, rb, end;
-    if (!gather_place(a, 128, cb, rb, end)) return;
+    if (!gather_place(a, a.C, 128, cb, rb, end)) return;
     const int c = cb * 128 + 8 * sub;
     int t[kActRows];
     float none[kActRows];
@@ -189,11 +199,11 @@ template <class XT>
 static void gather(const RowsArgs &a, const XT *x, void *plain, bool plain_f32, const ActForm &row, const ActForm &col,
                    hipStream_t s) {
     if (plain) {
-        const dim3 grid((a.C + 127) / 128 * ((a.rows + 63) / 64));
+        auto grid = [&](int columns) { return dim3((columns + 127) / 128 * ((a.rows + 63) / 64)); };
         if (plain_f32)
-            hipLaunchKernelGGL((gather_plain<XT, float>), grid, dim3(256), 0, s, a, x, static_cast<float *>(plain));
+            hipLaunchKernelGGL((gather_plain<XT, float>), grid(plain_columns<float>(a.C)), dim3(256), 0, s, a, x, static_cast<float *>(plain));
         else
-            hipLaunchKernelGGL((gather_plain<XT, uint16_t>), grid, dim3(256), 0, s, a, x, static_cast<uint16_t *>(plain));
+            hipLaunchKernelGGL((gather_plain<XT, uint16_t>), grid(plain_columns<uint16_t>(a.C)), dim3(256), 0, s, a, x, static_cast<uint16_t *>(plain));
     }
     const unsigned nkb = (a.C + 127) / 128;
     if constexpr (std::is_same_v<XT, uint16_t>)
