@@ -270,14 +270,16 @@ static void grad(const ProductArgs &p, const GroupArgs &g, bool ahead, hipStream
 // bf16: 256 x 256 where three rounds of the CUs are full or one nearly is, as one such tile of 1 to 64 steps reads half of
 // what four of 128 x 128 do (64 experts of 2048 x 1536, mean 16, 96, 512 and 1024 rows: 99 111 178 258 us, 128 x 128:
 // 118 131 202 294).  Fewer tiles leave CUs without work in the last round (64 of 512 x 768, mean 512 and 1024: 45 and
-// 76 us, 128 x 128: 43 and 62; 16 of 1024 x 1024, mean 1024: 49 and 42).  float32 results, whose operands are widened in registers:
+// 76 us, 128 x 128: 43 and 62; 16 of 1024 x 1024, mean 1024: 49 and 42), and so do results that cover
+// less than 3/4 of their tiles (128 of 128 x 2048, mean 12, 96 and 384: 36 45 81 us, 128 x 128: 31 38 70; of 384 x 2048: 66 77 124
+// and 69 77 117; of 640 x 2048, 5/6: 94 114 189 and 115 130 192).  float32 results, whose operands are widened in registers:
 // 128 x 128 was best of 128 x 64, 256 x 64, 128 x 256 and 256 x 128 (128 of 1536 x 2048, mean 94: 417 us, the last two 432 and 467).
 // Reading ahead gains up to some 512 rows a group (32 of 4096 x 7168, mean 48, 256, 512 and 1024: 635 657 827 1151 us without,
 // 545 572 761 1144 with it) and from two runs of experts on (8 to 15 experts: alike, or slower).
 hipError_t launch_expert_weight_grad(const ProductArgs &p, const GroupArgs &g, float mean, int out, hipStream_t s) {
     const bool ahead = g.off && g.n >= 2 * kAheadExperts && mean <= 1024;
     const float largest = static_cast<float>((p.M + 255) / 256) * ((p.R + 255) / 256) * g.n;   // tiles of 256 x 256
-    const bool full = largest >= 768 || (largest > 128 && largest <= 224);
+    const bool full = (largest >= 768 || (largest > 128 && largest <= 224)) && static_cast<float>(p.M) * p.R * g.n >= 0.75f * 65536 * largest;
     if (out == 0 && full) grad<8, 4, 2, 4, false, 0>(p, g, ahead, s);
     else if (out == 0) grad<4, 4, 2, 2, false, 0>(p, g, ahead, s);
     else if (out == 1) grad<4, 4, 2, 2, true, 1>(p, g, ahead, s);
