@@ -5,7 +5,7 @@
 // All of these move memory and compute little: the bound is HBM, and for the 8-bit forms the vector units, where a value is
 // handled in its own register (float32, weights); bf16 rows without weights are handled in pairs.  8192 tokens of 7168 channels, 8
 // experts each (62000 to 65536 rows, 78000 to 82000 with padding), replayed over buffers that no cache holds: both forms 270 us, 4.6 TB/s, the row form
-// 190, plain rows 285; back to the tokens 204 us, 5.1 TB/s; the gates 190.
+// 190, plain rows 285; back to the tokens 202 us, 5.2 TB/s; the gates 190.
 #include "act_tile.h"
 #include "gemm_tile.h"
 

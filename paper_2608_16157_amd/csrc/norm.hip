@@ -11,8 +11,8 @@
 //   d_post = scale g A,  d_gate = scale post A,  d_pre = B
 //
 // A row lies in the registers of its LANES threads (8 CH channels a thread, LANES x 8 channels a step), so each matrix
-// is read once.  Row sums: lanes of a wave, then the waves in order through LDS.  Column sums: a thread's own over the rows
-// of its workgroup, then over the workgroups in order, in float64.
+// is read once.  Row sums: lanes of a wave, then the waves in order through LDS.  Column sums: a thread's own over its
+// rows, where a workgroup has several at once over these, then over the workgroups in order, in float64.
 //
 // The bound is HBM: forward with a norm on both sides 8192 x 7168 bf16 112 us, 4.7 TB/s; backward 150 us and 5 for the join, 4.6 TB/s.
 #include "act_tile.h"
@@ -336,7 +336,21 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES == 1024 ? 4 : 3) v
         }
     }
     if (!a.parts) return;
-    float *mine = a.parts + static_cast<size_t>(part) * 2 * a.C;
+    float *mine = a.parts + static_cast<size_t>(blockIdx.x) * 2 * a.C;
+    if constexpr (kRows > 1) {   // the rows' waves, in order
+        static_assert(CH == 1 && LANES * 16 == 4 * 256);
+        __shared__ __attribute__((aligned(16))) float rows[kRows][2][LANES * 8];
+        store8(rows[threadIdx.x / LANES][0] + lane * 8, sa[0]);
+        store8(rows[threadIdx.x / LANES][1] + lane * 8, sb[0]);
+        __syncthreads();
+        const int which = threadIdx.x / (2 * LANES), at = 4 * (threadIdx.x % (2 * LANES));
+        if (at >= a.C) return;
+        floatx4_t sum = *reinterpret_cast<const floatx4_t *>(&rows[0][which][at]);
+#pragma unroll
+        for (int r = 1; r < kRows; ++r) sum += *reinterpret_cast<const floatx4_t *>(&rows[r][which][at]);
+        *reinterpret_cast<floatx4_t *>(mine + which * a.C + at) = sum;
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < CH; ++i)
         if (in[i]) {
@@ -353,16 +367,18 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES == 1024 ? 4 : 3) v
         }
 }
 
-// Column sums of the parts: 64 columns of A or B per workgroup, 16 runs of parts by 16 threads of 4 columns.
-__global__ __launch_bounds__(256) void block_norm_join(NormArgs a, bool w_f32, float *d_pre, float *d_post, float *d_gate) {
-    __shared__ double sums[16][64];
+// Column sums of the parts: 64 columns of A or B per workgroup, RUNS runs of parts by 16 threads of 4 columns.  Few columns have few
+// workgroups and up to 1024 parts: 64 runs there (27648 x 368, with the waves' sums joined before: 52 -> 37 us; from 2048 columns on 16 are better).
+template <int RUNS>
+__global__ __launch_bounds__(16 * RUNS) void block_norm_join(NormArgs a, bool w_f32, float *d_pre, float *d_post, float *d_gate) {
+    __shared__ double sums[RUNS][64];
     const int run = threadIdx.x / 16, col = blockIdx.x * 64 + 4 * (threadIdx.x % 16);
     const bool second = blockIdx.y == 1;
     double v[4] = {0.0, 0.0, 0.0, 0.0};
     if (col < a.C) {
         const float *p = a.parts + (second ? a.C : 0) + col;
 #pragma unroll 8
-        for (int i = run; i < a.n_parts; i += 16) {
+        for (int i = run; i < a.n_parts; i += RUNS) {
             const float4 f = *reinterpret_cast<const float4 *>(p + static_cast<size_t>(i) * 2 * a.C);
             v[0] += f.x;
             v[1] += f.y;
@@ -377,7 +393,7 @@ __global__ __launch_bounds__(256) void block_norm_join(NormArgs a, bool w_f32, f
     if (threadIdx.x >= 64 || c >= a.C) return;
     double s = 0.0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s += sums[i][threadIdx.x];
+    for (int i = 0; i < RUNS; ++i) s += sums[i][threadIdx.x];
     if (second) {
         if (d_pre) d_pre[c] = static_cast<float>(s);
         return;
@@ -404,7 +420,7 @@ static int norm_blocks(int T, int C, bool back) {
     const NormShape n = norm_shape(C);
     return std::min((T + n.rows - 1) / n.rows, (back || n.lanes == 1024 ? 256 : 384) * 1024 / std::max(n.lanes, 256));
 }
-int norm_parts(int T, int C) { return norm_blocks(T, C, true) * norm_shape(C).rows; }
+int norm_parts(int T, int C) { return norm_blocks(T, C, true); }
 
 template <class XT, class YT, bool BACK>
 static void norm_go(const NormArgs &a, bool w_f32, hipStream_t s) {
@@ -443,8 +459,9 @@ hipError_t launch_block_norm(const NormArgs &a, bool x_f32, bool y_f32, bool w_f
 hipError_t launch_block_norm_backward(const NormArgs &a, bool x_f32, bool y_f32, bool w_f32, float *d_pre, float *d_post,
                                       float *d_gate, hipStream_t s) {
     if (a.T > 0) norm_types<true>(a, x_f32, y_f32, w_f32, s);
-    if (a.parts)
-        hipLaunchKernelGGL(block_norm_join, dim3((a.C + 63) / 64, 2), dim3(256), 0, s, a, w_f32, d_pre, d_post, d_gate);
+    const dim3 grid((a.C + 63) / 64, 2);
+    if (a.parts && a.C <= 1024) hipLaunchKernelGGL(block_norm_join<64>, grid, dim3(1024), 0, s, a, w_f32, d_pre, d_post, d_gate);
+    else if (a.parts) hipLaunchKernelGGL(block_norm_join<16>, grid, dim3(256), 0, s, a, w_f32, d_pre, d_post, d_gate);
     return hipGetLastError();
 }
 
