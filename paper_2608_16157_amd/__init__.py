@@ -820,6 +820,38 @@ def _codes_arg(dev: int, c, name: str, rows: int, cols: int, optional: bool = Fa
     return dev, ctypes.byref(ft_act_codes_t(codes, scales))
 
 
+def _in_rows(t: torch.Tensor, stream) -> torch.Tensor:
+    """A copy of a strided 2-D tensor of bytes in rows.  The transpose of rows goes through the weight transpose where its
+    sizes are ones of a weight: 7168 x 36864 in 112 us, 2048 x 28160 in 19, in 1032 and 259 by torch's copy, which moves single
+    bytes.  Small ones wait for the host, which takes longer here: 1024 x 1024 12.7 us, 6.8 by torch's copy."""
+    rows, kp = t.shape
+    if t.is_cuda and t.numel() >= 1 << 22 and t.t().is_contiguous() and rows % 128 == 0 and kp % 128 == 0 and \
+            max(rows, kp) <= 65536 and t.data_ptr() % 16 == 0:
+        new = lambda *shape, dtype: torch.empty(*shape, dtype=dtype, device=t.device)
+        out = new(rows, kp, dtype=torch.uint8)
+        unused = {"s": new(kp // 128, rows // 128, dtype=torch.float32)}, {"s": new(rows // 128, kp // 128, dtype=torch.float32)}
+        ft_linear_transpose(kp, rows, {"w": t.t(), **unused[0]}, {"w": out, **unused[1]}, stream)
+        return out
+    return t.contiguous()
+
+
+def _laid_out(c, stream):
+    """An input form whose tensors are strided views, as quantising a transposed matrix leaves them, in rows: a copy that
+    lives on the call's stream.  Everything else goes on as it is, to be refused where it does not fit."""
+    if not isinstance(c, ActCodes) or not all(isinstance(t, torch.Tensor) for t in (c.codes, c.scales)):
+        return c
+    if c.codes.is_contiguous() and c.scales.is_contiguous():
+        return c
+    kp = _pad128(c.cols)
+    if c.codes.shape != (c.rows, kp) or c.scales.shape != (kp // 128, _pad128(c.rows)):
+        return c
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, c.codes.device)
+    with torch.cuda.stream(stream):   # None: no change
+        rows = [t if t.is_contiguous() else _in_rows(t, stream) for t in (c.codes, c.scales)]
+    return ActCodes.of(*rows, c.rows, c.cols)
+
+
 def _need_sizes(T: int, *features: int) -> None:
     """Sizes the library refuses (FT_ERR_SHAPE) would make the element counts here meaningless."""
     if not 0 <= T <= 1048576 or any(not 16 <= f <= 65536 or f % 16 for f in features):
@@ -906,12 +938,14 @@ def ft_linear_transpose(out_features: int, in_features: int, weight: dict, weigh
 
 def ft_linear_weight_grad(out_features: int, in_features: int, T: int, dy_col: ActCodes, x_col: ActCodes,
                           dw: torch.Tensor, accumulate: bool = False, stream=None) -> None:
-    """``dw``: float32 or bfloat16 [out_features][in_features]."""
+    """``dw``: float32 or bfloat16 [out_features][in_features].  ``dy_col``, ``x_col``: forms whose tensors are strided
+    views (a transposed matrix was quantised) are brought into rows by the call, at the price of a copy."""
     N, K, T = int(out_features), int(in_features), int(T)
     _need_sizes(T, N, K)
     dev, out = _arg(-1, dw, "dw", _FLOAT_TYPES, N * K)
     yp = xp = None
     if T > 0:
+        dy_col, x_col = _laid_out(dy_col, stream), _laid_out(x_col, stream)
         dev, yp = _codes_arg(dev, dy_col, "dy_col", N, T)
         dev, xp = _codes_arg(dev, x_col, "x_col", K, T)
     st = _on(dev, load().ft_linear_weight_grad, N, K, T, yp, xp, out, _FLOATS[dw.dtype], 1 if accumulate else 0, stream)
@@ -1253,12 +1287,14 @@ def ft_expert_linear_transpose(n: int, out_features: int, in_features: int, weig
 
 def ft_expert_weight_grad(desc: dict, out_features: int, in_features: int, dy_col: ActCodes, x_col: ActCodes,
                           sort: SortBuffers, T: int, dw: torch.Tensor, accumulate: bool = False, stream=None) -> None:
-    """``dw``: float32 or bfloat16 [local][out_features][in_features]."""
+    """``dw``: float32 or bfloat16 [local][out_features][in_features].  ``dy_col``, ``x_col``: strided views are brought
+    into rows by the call, as in ft_linear_weight_grad."""
     d, N, K, T = _sort_desc(desc), int(out_features), int(in_features), int(T)
     _need_tokens(d, T, N, K)
     dev, out = _arg(-1, dw, "dw", _FLOAT_TYPES, d.local * N * K)
     yp = xp = sp = None
     if T > 0:
+        dy_col, x_col = _laid_out(dy_col, stream), _laid_out(x_col, stream)
         dev, yp = _codes_arg(dev, dy_col, "dy_col", N, d.rows)
         dev, xp = _codes_arg(dev, x_col, "x_col", K, d.rows)
         dev, sp = _groups_arg(dev, d, sort)
