@@ -252,9 +252,8 @@ def prepare(case, seed):
             wt = torch.zeros(n, K, _up128(N), dtype=torch.uint8, device="cuda")
             wt[:, :, :N] = w.transpose(1, 2)[:, :K]
             dy = _activations(rows, N, g).float() * 1e-3 * real
-            column_form = lambda v: tuple(t.contiguous() for t in _quantize(v.t()))   # in rows, as the calls take them
-            st |= {"wt": wt, "st": s.transpose(1, 2).contiguous(), "dy_row": _quantize(dy), "dy_col": column_form(dy),
-                   "x_col": column_form((_activations(rows, K, g) * real).float()),
+            st |= {"wt": wt, "st": s.transpose(1, 2).contiguous(), "dy_row": _quantize(dy), "dy_col": _quantize(dy.t()),
+                   "x_col": _quantize((_activations(rows, K, g) * real).float().t()),
                    "dx": torch.zeros(rows, K, dtype=torch.bfloat16, device="cuda"),
                    "dw": torch.empty(n, N, K, dtype=_DTYPES[case["out"]], device="cuda")}
     return st
