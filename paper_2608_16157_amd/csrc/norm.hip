@@ -94,6 +94,12 @@ __device__ __forceinline__ void values8(const Raw8<T> &r, float *v) {
         v[q] = __uint_as_float(sizeof(T) == 4 ? w[q] : q % 2 ? w[q / 2] & 0xFFFF0000u : w[q / 2] << 16);
 }
 
+// Threads past a row's end hold its last channels, which may be infinite: both factors are taken away.
+__device__ __forceinline__ void add_square(bool in, float v, float &s) {
+    const float own = in ? v : 0.0f;
+    s = fmaf(own, own, s);
+}
+
 template <class XT, class YT, int LANES, int CH>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES == 1024 ? 4 : 5) void block_norm(NormArgs a, bool w_f32) {
     constexpr int kRows = LANES < 256 ? 256 / LANES : 1;   // rows of a workgroup at once
@@ -151,7 +157,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES == 1024 ? 4 : 5) v
 #pragma unroll
                 for (int i = 0; i < CH; ++i)
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) s[0] = fmaf(in[i] ? b[i][q] : 0.0f, b[i][q], s[0]);
+                    for (int q = 0; q < 8; ++q) add_square(in[i], b[i][q], s[0]);
                 row_sums<LANES, 1>(s, buf, turn);
                 h *= over_rms(s[0], a);
             }
@@ -169,7 +175,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES == 1024 ? 4 : 5) v
 #pragma unroll
         for (int i = 0; i < CH; ++i)
 #pragma unroll
-            for (int q = 0; q < 8; ++q) s[0] = fmaf(in[i] ? x[i][q] : 0.0f, x[i][q], s[0]);
+            for (int q = 0; q < 8; ++q) add_square(in[i], x[i][q], s[0]);
         row_sums<LANES, 1>(s, buf, turn);
         const float rr = over_rms(s[0], a);
 #pragma unroll
