@@ -769,7 +769,9 @@ ft_status_t ft_expert_weight_grad(const ft_sort_desc_t *desc, int32_t out_featur
  *              (FT_DT_BF16 or FT_DT_F32 each);  eps >= 0 and scale finite (FT_ERR_SHAPE otherwise)
  *   params     pre, post, gate [C], token_gate [T] float32; NULL: ones
  * Everything is computed in float32 and rounded once: n is of r before r's rounding.  Sums of squares are float32 too:
- * values past 2^64 / sqrt(C) in a row leave its norm 0; a row of zeros with eps 0 has none (NaN).
+ * values past 2^64 / sqrt(C) in a row leave its norm 0; a row with mean v^2 + eps below 2^-126, rms(v) 2^-63, loses the
+ * accuracy of 1 / rms, and one whose squares all vanish without eps (values below 2^-75) has none: infinities, or NaN for a
+ * row of zeros.
  */
 typedef struct {
     int32_t channels, x_dtype, y_dtype, w_dtype, post_norm;
