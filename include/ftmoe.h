@@ -647,6 +647,10 @@ ft_status_t ft_router_backward(const ft_balance_desc_t *desc, const float *logit
  *   backward   ft_expert_gather of dy with topk_w (both forms), ft_expert_gate_grad (the d_topk_w of
  *              ft_router_backward); ft_expert_linear and ft_expert_weight_grad (down); ft_swiglu_backward over the rows;
  *              ft_expert_linear and ft_expert_weight_grad (gate and up); ft_expert_combine without weights (dx)
+ * The two SwiGLU calls know no groups: called with T = rows they read and write all rows of the capacity, those behind
+ * the last group too, whatever these hold (no call of a step reads what they leave there).  Where few of the experts are here and
+ * rows is what any routing needs, that is several times the groups' rows; a capacity near the expected share costs less, and
+ * `dropped` says when it was too small.
  *
  * The rows' layout (host struct, read during the call only; the same for every call of a step):
  *   n_experts, top_k   as in ft_moe_desc_t: 1..1024, 1..min(n_experts, 64)
