@@ -671,7 +671,9 @@ typedef struct {
  * The tables (device pointers, caller-owned).  Group e = 0 .. local - 1 belongs to expert first + e.
  *   row_pair [rows]     pair p = t * top_k + j of a row; -1: no pair (a group's padding, rows behind the last group)
  *   pair_row [T*top_k]  row of a pair; -1: none (an expert that is not here, a masked token, no place)
- *   off      [local+1]  group e is rows [off[e], off[e+1]), pairs first, in ascending order; off[local] ends the last
+ *   off      [local+1]  group e is rows [off[e], off[e+1]), pairs first, in ascending order; off[local] ends the last.  A
+ *                       group ends at the first multiple of align behind its pairs, without pairs it has no rows:
+ *                       ft_expert_linear sizes its grid by that, and leaves out rows past what T tokens can fill so
  *   count    [local]    its rows with a pair
  *   dropped  [1]        pairs of local experts that found no place: when the capacity is used up, the
  *                       pairs left of that expert and all of the later ones
