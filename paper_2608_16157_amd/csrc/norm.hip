@@ -14,7 +14,8 @@
 // is read once.  Row sums: lanes of a wave, then the waves in order through LDS.  Column sums: a thread's own over its
 // rows, where a workgroup has several at once over these, then over the workgroups in order, in float64.
 //
-// The bound is HBM: forward with a norm on both sides 8192 x 7168 bf16 112 us, 4.7 TB/s; backward 150 us and 5 for the join, 4.6 TB/s.
+// The bound is HBM: forward with a norm on both sides 8192 x 7168 bf16 103 to 112 us, 4.7 to 5.1 TB/s; backward 151 us, 5 of them the
+// join, 4.7 TB/s.
 #include "act_tile.h"
 
 #include <algorithm>
@@ -205,7 +206,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES == 1024 ? 4 : 5) v
 // A row's channels of a thread; up to 8192 channels the next row's are requested before the sums of this one are waited for: a
 // workgroup of 1024 threads fills a CU, and without its next row on the way nothing is (8192 x 7168: 324 us; 16 channels a
 // thread and half the threads spill).  Up to 16384 channels the weights are read again for every row and the column sums
-// lie in LDS (3500 x 16384: 517 us with all of it in registers, 388 without the weights, 246 so); beyond, registers spill.
+// lie in LDS (3500 x 16384: 517 us with all of it in registers, 388 without the weights, 250 so); beyond, registers spill (1700 x
+// 32768: 2479 us, the forward pass 596).
 template <class XT, class YT, int LANES, int CH>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES, LANES == 1024 ? 4 : 3) void block_norm_backward(NormArgs a, bool w_f32) {
     constexpr int kRows = LANES < 256 ? 256 / LANES : 1;
